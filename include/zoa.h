@@ -405,6 +405,107 @@ zoa_status zoa_onebit_allreduce_static(const float *const *z, float *const *delt
 size_t zoa_static_scratch_slots(void);
 const char *zoa_static_last_error(void);
 
+/* ---- Operators of a low-bit student --------------------------------------------
+ * What produces the gradients of a step when the model's linear layers run in 4
+ * bits and a stored teacher gives the loss: 4-bit microscaled matrices, their
+ * products, and distillation from a teacher's top logits.  No handle: every call works on buffers the
+ * caller owns, on the current device, allocates nothing, checks its arguments before anything is
+ * enqueued (ZOA_ERR_ARG), enqueues on `stream` and does not synchronise.  A call
+ * that fails returns a status; its text is zoa_ops_last_error() of the same thread.
+ * Calls may be made from several threads.  (The paper has no counterpart to them.)
+ *
+ * Element types of the plain matrices: binary32, binary16, bfloat16.  `ld` is the
+ * distance between rows in elements; neighbours of a row are contiguous.  Rows
+ * that are 16-byte aligned take the 128-bit paths, any other alignment of the
+ * element type works.  Sizes of zero do nothing. */
+typedef enum { ZOA_F32 = 0, ZOA_F16 = 1, ZOA_BF16 = 2 } zoa_dtype;
+
+/* 4-bit microscaled form of a matrix: E2M1 elements (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives) with one E8M0 scale, a power of two, per 32 neighbours of a row
+ * (the last block of a row may be shorter).  With a = max |x_i| of the block:
+ *   scale = 2^max(floor(log2 a) - 2, -127),   code_i = x_i / scale rounded to the
+ *   nearest element, ties to the even code, at most 6 in magnitude.
+ * A block of zeros has scale 2^-127.  A block with a NaN or an infinity reads back
+ * as NaN, and so does every product that touches it.
+ * The form is one buffer of zoa_mx4_size(rows, cols) bytes (0 for an empty or
+ * too large matrix: a side is at most 2^30), 16-byte aligned, whose layout belongs to the library: tiles
+ * of 128 rows by 256 columns, scales before codes.  Rounding the values that a form stands
+ * for gives those values again, so zoa_mx4_dequantize and zoa_mx4_quantize also
+ * convert from and to any other layout without loss.
+ * zoa_mx4_quantize: out (may be NULL) receives the form of x [rows, cols], out_t
+ * (may be NULL, not both) that of its transpose [cols, rows], blocks along x's
+ * columns; both come from one read of x. */
+size_t zoa_mx4_size(size_t rows, size_t cols);
+zoa_status zoa_mx4_quantize(const void *x, int dtype, size_t rows, size_t cols, size_t ld, void *out, void *out_t,
+                            void *stream);
+zoa_status zoa_mx4_dequantize(const void *q, size_t rows, size_t cols, void *out, int dtype, size_t ld, void *stream);
+
+/* out[i, j] = sum over k of a[i, k] b[j, k]: a is the form of an [m, k] matrix, b of an
+ * [n, k] one, out [m, n] of the given type; sums in binary32, one rounding at the
+ * end.  (b is a linear layer's weight as it is usually kept, [out, in].)  k = 0
+ * gives zeros.  The order of a sum depends on the sizes alone: equal calls give equal bits. */
+zoa_status zoa_mx4_matmul(const void *a, const void *b, size_t m, size_t n, size_t k, void *out, int dtype, size_t ld,
+                          void *stream);
+
+/* A linear layer on real activations: out = Q(x) b^T, Q being the rounding of
+ * zoa_mx4_quantize.  work: (device) zoa_mx4_linear_work(m, n, k) bytes, 16-byte aligned, for
+ * the 4-bit form of x (NULL where that is 0: few rows are rounded inside the
+ * product).  x and out have the same type. */
+size_t zoa_mx4_linear_work(size_t m, size_t n, size_t k);
+zoa_status zoa_mx4_linear(const void *x, int dtype, size_t m, size_t k, size_t ldx, const void *b, size_t n, void *out,
+                          size_t ld, void *work, void *stream);
+
+/* Distillation from a teacher's top logits, row by row.  With z the student's
+ * logits of a row [vocab], (i_k, t_k), k < top, the teacher's listed tokens and
+ * logits, T the temperature:
+ *   q = softmax(z / T) over the vocabulary
+ *   p = softmax of the listed t_k / T              (teacher_lse NULL)
+ *   soft = sum_k p_k (log p_k - log q_{i_k})
+ * or, with teacher_lse = log sum exp(t / T) over the teacher's whole vocabulary, its
+ * true probabilities with everything unlisted as one more outcome:
+ *   p_k = exp(t_k / T - teacher_lse),  p_r = max(0, 1 - sum p_k),  q_r = sum of q over unlisted tokens
+ *   soft = sum_k p_k (log p_k - log q_{i_k}) + p_r (log p_r - log q_r)
+ * and with y the row's label and w its weight (1 where row_weight is NULL)
+ *   loss = w (soft_weight T^2 soft + hard_weight (log sum exp z - z_y))
+ *   grad = d loss / d z
+ * index: int32 [rows, top]; an entry outside [0, vocab) is skipped (shorter lists end
+ * in -1), a token listed twice counts with both probabilities, a row with no entry
+ * left, or none above -inf, has no soft part.  A term with p = 0 is 0.
+ * labels (may be NULL): int32 [rows]; a row whose label is outside [0, vocab) has
+ * no hard part.  A row of weight 0 gives loss 0 and gradient 0 whatever it holds.
+ * Logits of -inf are tokens masked out (q = 0, gradient 0); a row of nothing else gives loss 0 and gradient 0.  The p_r term is left out of
+ * a row whose q_r is 0 or below 1e-30.  A NaN or +inf logit makes
+ * its row NaN.  All sums in binary32.
+ * zoa_distill_topk: loss (binary32 [rows]), and, where they are not NULL, grad
+ * [rows, vocab] (the logits' type; may be the logits themselves with the same ld: they are then replaced) and stats
+ * (binary32 [rows, 4], for the next call).  teacher has the logits' type.
+ * zoa_distill_topk_backward: grad of grad_loss[row] * loss[row] from the same
+ * inputs and the stats of the forward call, with no second reduction. */
+typedef struct {
+    const void *logits;      /* (device) [rows, vocab] */
+    const int32_t *index;    /* (device) [rows, top], rows contiguous */
+    const void *teacher;     /* (device) [rows, top], rows contiguous */
+    const float *teacher_lse;/* (device) [rows] or NULL */
+    const int32_t *labels;   /* (device) [rows] or NULL */
+    const float *row_weight; /* (device) [rows] or NULL */
+    size_t rows, vocab, top;
+    size_t ld_logits;        /* elements between rows of logits */
+    int dtype;               /* of logits, teacher and grad */
+    float temperature, soft_weight, hard_weight;
+} zoa_distill_args;
+zoa_status zoa_distill_topk(const zoa_distill_args *args, float *loss, float *stats, void *grad, size_t ld_grad, void *stream);
+zoa_status zoa_distill_topk_backward(const zoa_distill_args *args, const float *stats, const float *grad_loss, void *grad,
+                                     size_t ld_grad, void *stream);
+
+/* Text of the last error of one of these calls on this thread (never NULL).
+ * zoa_ops_set_option: ZOA_OPT_WAIT_LIMIT_MS and ZOA_OPT_TEST_STOP_AFTER_TILES for the
+ * product kernels of this process, with the meaning and the defaults they have on a handle.
+ * zoa_ops_check_device: waits for the device; ZOA_ERR_DEVICE if a product kernel gave up on a
+ * bounded wait since the last check (its result is undefined; the condition is cleared). */
+const char *zoa_ops_last_error(void);
+zoa_status zoa_ops_set_option(int option, int value);
+zoa_status zoa_ops_check_device(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,6 +28,14 @@ class Stats(C.Structure):
                 ("t_sync", C.c_int64), ("gamma_sum", C.c_double)]
 
 
+class DistillArgs(C.Structure):
+    """zoa_distill_args of include/zoa.h."""
+    _fields_ = [("logits", C.c_void_p), ("index", C.c_void_p), ("teacher", C.c_void_p), ("teacher_lse", C.c_void_p),
+                ("labels", C.c_void_p), ("row_weight", C.c_void_p), ("rows", C.c_size_t), ("vocab", C.c_size_t),
+                ("top", C.c_size_t), ("ld_logits", C.c_size_t), ("dtype", C.c_int), ("temperature", C.c_float),
+                ("soft_weight", C.c_float), ("hard_weight", C.c_float)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: run `python -m paper_2202_06009_b200.build` "
@@ -82,6 +90,17 @@ def _load():
         "zoa_onebit_allreduce_static": ([C.POINTER(p), C.POINTER(p), p, p, C.c_size_t, C.c_int, C.c_int, p], C.c_int),
         "zoa_static_scratch_slots": ([], C.c_size_t),
         "zoa_static_last_error": ([], C.c_char_p),
+        "zoa_mx4_size": ([C.c_size_t, C.c_size_t], C.c_size_t),
+        "zoa_mx4_quantize": ([p, C.c_int, C.c_size_t, C.c_size_t, C.c_size_t, p, p, p], C.c_int),
+        "zoa_mx4_dequantize": ([p, C.c_size_t, C.c_size_t, p, C.c_int, C.c_size_t, p], C.c_int),
+        "zoa_mx4_matmul": ([p, p, C.c_size_t, C.c_size_t, C.c_size_t, p, C.c_int, C.c_size_t, p], C.c_int),
+        "zoa_mx4_linear_work": ([C.c_size_t, C.c_size_t, C.c_size_t], C.c_size_t),
+        "zoa_mx4_linear": ([p, C.c_int, C.c_size_t, C.c_size_t, C.c_size_t, p, C.c_size_t, p, C.c_size_t, p, p], C.c_int),
+        "zoa_distill_topk": ([C.POINTER(DistillArgs), p, p, p, C.c_size_t, p], C.c_int),
+        "zoa_distill_topk_backward": ([C.POINTER(DistillArgs), p, p, p, C.c_size_t, p], C.c_int),
+        "zoa_ops_last_error": ([], C.c_char_p),
+        "zoa_ops_set_option": ([C.c_int, C.c_int], C.c_int),
+        "zoa_ops_check_device": ([], C.c_int),
     }
     for name, (argtypes, restype) in sigs.items():
         fn = getattr(lib, name)
@@ -321,3 +340,52 @@ def zoa_onebit_allreduce_static(z_ptrs, delta_w_ptrs, delta_s_ptr, z_bar_ptr, n,
 
 def zoa_static_scratch_slots():
     return lib.zoa_static_scratch_slots()
+
+
+# -- operators without a handle ---------------------------------------------------
+F32, F16, BF16 = 0, 1, 2
+
+
+def _check_ops(status):
+    if status != OK:
+        raise ZoaError(status, lib.zoa_ops_last_error().decode())
+
+
+def zoa_mx4_size(rows, cols):
+    return lib.zoa_mx4_size(rows, cols)
+
+
+def zoa_mx4_quantize(x_ptr, dtype, rows, cols, ld, out_ptr, out_t_ptr, stream=0):
+    _check_ops(lib.zoa_mx4_quantize(x_ptr, dtype, rows, cols, ld, out_ptr, out_t_ptr, stream))
+
+
+def zoa_mx4_dequantize(q_ptr, rows, cols, out_ptr, dtype, ld, stream=0):
+    _check_ops(lib.zoa_mx4_dequantize(q_ptr, rows, cols, out_ptr, dtype, ld, stream))
+
+
+def zoa_mx4_matmul(a_ptr, b_ptr, m, n, k, out_ptr, dtype, ld, stream=0):
+    _check_ops(lib.zoa_mx4_matmul(a_ptr, b_ptr, m, n, k, out_ptr, dtype, ld, stream))
+
+
+def zoa_mx4_linear_work(m, n, k):
+    return lib.zoa_mx4_linear_work(m, n, k)
+
+
+def zoa_mx4_linear(x_ptr, dtype, m, k, ldx, b_ptr, n, out_ptr, ld, work_ptr, stream=0):
+    _check_ops(lib.zoa_mx4_linear(x_ptr, dtype, m, k, ldx, b_ptr, n, out_ptr, ld, work_ptr, stream))
+
+
+def zoa_distill_topk(args, loss_ptr, stats_ptr, grad_ptr, ld_grad, stream=0):
+    _check_ops(lib.zoa_distill_topk(C.byref(args), loss_ptr, stats_ptr, grad_ptr, ld_grad, stream))
+
+
+def zoa_distill_topk_backward(args, stats_ptr, grad_loss_ptr, grad_ptr, ld_grad, stream=0):
+    _check_ops(lib.zoa_distill_topk_backward(C.byref(args), stats_ptr, grad_loss_ptr, grad_ptr, ld_grad, stream))
+
+
+def zoa_ops_set_option(option, value):
+    _check_ops(lib.zoa_ops_set_option(option, value))
+
+
+def zoa_ops_check_device():
+    _check_ops(lib.zoa_ops_check_device())
