@@ -455,6 +455,19 @@ size_t zoa_mx4_linear_work(size_t m, size_t n, size_t k);
 zoa_status zoa_mx4_linear(const void *x, int dtype, size_t m, size_t k, size_t ldx, const void *b, size_t n, void *out,
                           size_t ld, void *work, void *stream);
 
+/* The layer's training step, the rounding's own derivative taken as 1.
+ * zoa_mx4_linear_forward: y [m, n] = Q(x) Q(w)^T from real x [m, k] (of type x_type, as
+ * y) and w [n, k]; xt and wt receive the forms of x^T (zoa_mx4_size(k, m) bytes) and w^T
+ * (zoa_mx4_size(k, n)) for the next call; work: (device) zoa_mx4_size(m, k) + zoa_mx4_size(n, k) bytes.
+ * zoa_mx4_linear_backward: dx [m, k] = Q(dy) Q(w^T)^T and dw [n, k] = Q(dy^T) Q(x^T)^T from
+ * dy [m, n]; either may be NULL if it is not wanted; work: (device) zoa_mx4_size(m, n) +
+ * zoa_mx4_size(n, m) bytes.  All forms and work areas 16-byte aligned. */
+zoa_status zoa_mx4_linear_forward(const void *x, int x_type, size_t ldx, const void *w, int w_type, size_t ldw, size_t m,
+                                  size_t n, size_t k, void *y, size_t ldy, void *xt, void *wt, void *work, void *stream);
+zoa_status zoa_mx4_linear_backward(const void *dy, int dy_type, size_t ld_dy, size_t m, size_t n, size_t k, const void *xt,
+                                   const void *wt, void *dx, int dx_type, size_t ld_dx, void *dw, int dw_type, size_t ld_dw,
+                                   void *work, void *stream);
+
 /* Distillation from a teacher's top logits, row by row.  With z the student's
  * logits of a row [vocab], (i_k, t_k), k < top, the teacher's listed tokens and
  * logits, T the temperature:

@@ -96,8 +96,13 @@ def _load():
         "zoa_mx4_matmul": ([p, p, C.c_size_t, C.c_size_t, C.c_size_t, p, C.c_int, C.c_size_t, p], C.c_int),
         "zoa_mx4_linear_work": ([C.c_size_t, C.c_size_t, C.c_size_t], C.c_size_t),
         "zoa_mx4_linear": ([p, C.c_int, C.c_size_t, C.c_size_t, C.c_size_t, p, C.c_size_t, p, C.c_size_t, p, p], C.c_int),
-        "zoa_distill_topk": ([C.POINTER(DistillArgs), p, p, p, C.c_size_t, p], C.c_int),
-        "zoa_distill_topk_backward": ([C.POINTER(DistillArgs), p, p, p, C.c_size_t, p], C.c_int),
+        "zoa_mx4_linear_forward": ([p, C.c_int, C.c_size_t, p, C.c_int, C.c_size_t, C.c_size_t, C.c_size_t, C.c_size_t,
+                                    p, C.c_size_t, p, p, p, p], C.c_int),
+        "zoa_mx4_linear_backward": ([p, C.c_int, C.c_size_t, C.c_size_t, C.c_size_t, C.c_size_t, p, p, p, C.c_int, C.c_size_t,
+                                     p, C.c_int, C.c_size_t, p, p], C.c_int),
+        # a zoa_distill_args as a DistillArgs by reference, or as its bytes
+        "zoa_distill_topk": ([p, p, p, p, C.c_size_t, p], C.c_int),
+        "zoa_distill_topk_backward": ([p, p, p, p, C.c_size_t, p], C.c_int),
         "zoa_ops_last_error": ([], C.c_char_p),
         "zoa_ops_set_option": ([C.c_int, C.c_int], C.c_int),
         "zoa_ops_check_device": ([], C.c_int),
@@ -373,6 +378,17 @@ def zoa_mx4_linear_work(m, n, k):
 
 def zoa_mx4_linear(x_ptr, dtype, m, k, ldx, b_ptr, n, out_ptr, ld, work_ptr, stream=0):
     _check_ops(lib.zoa_mx4_linear(x_ptr, dtype, m, k, ldx, b_ptr, n, out_ptr, ld, work_ptr, stream))
+
+
+def zoa_mx4_linear_forward(x_ptr, x_type, ldx, w_ptr, w_type, ldw, m, n, k, y_ptr, ldy, xt_ptr, wt_ptr, work_ptr, stream=0):
+    _check_ops(lib.zoa_mx4_linear_forward(x_ptr, x_type, ldx, w_ptr, w_type, ldw, m, n, k, y_ptr, ldy, xt_ptr, wt_ptr, work_ptr,
+                                          stream))
+
+
+def zoa_mx4_linear_backward(dy_ptr, dy_type, ld_dy, m, n, k, xt_ptr, wt_ptr, dx_ptr, dx_type, ld_dx, dw_ptr, dw_type, ld_dw,
+                            work_ptr, stream=0):
+    _check_ops(lib.zoa_mx4_linear_backward(dy_ptr, dy_type, ld_dy, m, n, k, xt_ptr, wt_ptr, dx_ptr, dx_type, ld_dx, dw_ptr,
+                                           dw_type, ld_dw, work_ptr, stream))
 
 
 def zoa_distill_topk(args, loss_ptr, stats_ptr, grad_ptr, ld_grad, stream=0):

@@ -8,7 +8,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libzoa.so")
 SOURCES = ["zoa_kernels.cu", "zoa_pipeline.cu", "zoa_reduce_pipeline.cu", "zoa_server_pipeline.cu", "zoa_api.cu", "zoa_noalloc.cu",
            "zoa_ops.cu", "zoa_mx4_quantize.cu", "zoa_mx4_matmul.cu", "zoa_distill.cu"]
-HEADERS = ["zoa_device.cuh", "zoa_internal.h", "zoa_ring.cuh", "zoa_ops.h", "zoa_mx4.cuh", os.path.join("..", "..", "include", "zoa.h")]
+HEADERS = ["zoa_device.cuh", "zoa_internal.h", "zoa_ring.cuh", "zoa_ops.h", "zoa_async.cuh", "zoa_mx4.cuh", os.path.join("..", "..", "include", "zoa.h")]
 
 # The arithmetic contract needs IEEE division and square root, subnormals kept,
 # and no contraction of a multiply and an add into one fused operation.

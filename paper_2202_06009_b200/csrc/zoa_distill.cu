@@ -5,7 +5,10 @@
 //   m,  s = sum e_j,  s1 = sum f_j,  r = sum of e_j over unlisted j
 // and the gradient is, for coefficients that are the same for the whole row,
 //   unlisted j: cu e_j + cb f_j        listed j: ca e_j - c0 p_j + cb f_j        label: - ch more.
+#include "zoa_async.cuh"
 #include "zoa_ops.h"
+
+#include <type_traits>
 
 namespace zoa {
 namespace {
@@ -38,7 +41,7 @@ __device__ __forceinline__ float ex2(float x)
 }
 
 // Running sums of part of a row relative to its largest logit.
-struct Sums {
+struct alignas(16) Sums {
     float m, s, s1, r;
 };
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
@@ -54,50 +57,120 @@ __device__ __forceinline__ Sums join(const Sums &a, const Sums &b, float c)
     o.s1 = a.s1 * shrink(a.m, o.m, kLog2e) + b.s1 * shrink(b.m, o.m, kLog2e);
     return o;
 }
-__device__ __forceinline__ Sums shuffle_join(Sums a, float c)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Sums b;
-        b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-        b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-        b.s1 = __shfl_xor_sync(0xffffffffu, a.s1, o);
-        b.r = __shfl_xor_sync(0xffffffffu, a.r, o);
-        a = join(a, b, c);
-    }
-    return a;
-}
-
-template <int kWarps>
-__device__ __forceinline__ float block_sum(float v, float *scratch)
+__device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-    __syncthreads();
-    float t = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) t += scratch[w];
-    return t;
+    return v;
 }
-template <int kWarps>
-__device__ __forceinline__ float block_max(float v, float *scratch)
+__device__ __forceinline__ float warp_max(float v)      // passes over a NaN like fmaxf
 {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-    __syncthreads();
-    float t = scratch[0];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) t = fmaxf(t, scratch[w]);
-    return t;
+    float m;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    return m;
+}
+// The sums of a warp's threads: one change of base each, then plain sums.
+__device__ __forceinline__ Sums warp_join(const Sums &a, float c)
+{
+    Sums o;
+    o.m = warp_max(a.m);
+    const float f = shrink(a.m, o.m, c);
+    o.s = warp_sum(a.s * f);
+    o.r = warp_sum(a.r * f);
+    o.s1 = warp_sum(a.s1 * shrink(a.m, o.m, kLog2e));
+    return o;
 }
 
-// A row cut into 16-byte vectors: `head` elements before the first aligned address, then `vecs` vectors, then
-// `tail` elements.  Bit j + shift of the bitmap stands for element j, so that a vector's bits start at a multiple
-// of its length.
+__device__ __forceinline__ uint64_t pair(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t ex2_2(uint64_t y)
+{
+    float lo, hi;
+    unpair(y, lo, hi);
+    return pair(ex2(lo), ex2(hi));
+}
+
+// A 16-byte vector as pairs of binary32, and its largest element.
+template <typename T>
+struct Pairs {
+    static constexpr int kCount = 4;
+    static __device__ __forceinline__ void unpack(const uint4 &w, uint64_t *x)
+    {
+        float lo, hi;
+        unpack2<T>(w.x, lo, hi);
+        x[0] = pair(lo, hi);
+        unpack2<T>(w.y, lo, hi);
+        x[1] = pair(lo, hi);
+        unpack2<T>(w.z, lo, hi);
+        x[2] = pair(lo, hi);
+        unpack2<T>(w.w, lo, hi);
+        x[3] = pair(lo, hi);
+    }
+    static __device__ __forceinline__ uint32_t pack_pair(uint64_t v)
+    {
+        float lo, hi;
+        unpair(v, lo, hi);
+        return pack2<T>(lo, hi);
+    }
+    static __device__ __forceinline__ uint4 pack(const uint64_t *x)
+    {
+        return make_uint4(pack_pair(x[0]), pack_pair(x[1]), pack_pair(x[2]), pack_pair(x[3]));
+    }
+    using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+    static __device__ __forceinline__ T2 as2(uint32_t w) { return *reinterpret_cast<const T2 *>(&w); }
+    static __device__ __forceinline__ float largest(const uint4 &w)
+    {
+        const T2 m = __hmax2(__hmax2(as2(w.x), as2(w.y)), __hmax2(as2(w.z), as2(w.w)));
+        float lo, hi;
+        unpack2<T>(*reinterpret_cast<const uint32_t *>(&m), lo, hi);
+        return fmaxf(lo, hi);
+    }
+};
+template <>
+struct Pairs<float> {
+    static constexpr int kCount = 2;
+    static __device__ __forceinline__ void unpack(const uint4 &w, uint64_t *x)
+    {
+        x[0] = (uint64_t)w.y << 32 | w.x;
+        x[1] = (uint64_t)w.w << 32 | w.z;
+    }
+    static __device__ __forceinline__ uint4 pack(const uint64_t *x)
+    {
+        return make_uint4((uint32_t)x[0], (uint32_t)(x[0] >> 32), (uint32_t)x[1], (uint32_t)(x[1] >> 32));
+    }
+    static __device__ __forceinline__ float largest(const uint4 &w)
+    {
+        return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+    }
+};
+
+template <typename T> constexpr uint32_t kMinusInfBits = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00u : 0xFF80u;
+
+// A row's elements before the first 16-byte boundary (`head`), the vectors from there, the elements after the last.
+// Bit j + shift of the bitmap stands for element j, so that a vector's bits lie in one byte.
 template <typename T>
 struct RowCut {
     int head, vecs, tail, shift;
@@ -112,197 +185,365 @@ struct RowCut {
     }
 };
 
-constexpr int kStreamThreads = 512, kStreamWarps = kStreamThreads / 32;
+// One entry of a row's list.
+struct Entry {
+    int token;       // -1: skipped
+    float z;         // the student's logit; NaN bits never matter here
+    float p;         // the teacher's logit, then its probability
+};
 
-// One block per row; the row is read once for the sums and once more, from L2, for the gradient.
-template <typename T>
-__global__ void __launch_bounds__(kStreamThreads) distill_stream_kernel(const DistillArgs a)
+constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 8;
+constexpr int kBatch = 4;          // vectors a thread has in flight
+constexpr int kBlocksPerSm = 4;
+
+struct DistillShared {
+    unsigned long long exchange;
+    Sums part[kWarps];
+    Sums theirs[kMaxCluster];
+    float mass, soft;
+    int any, twice, gave_up;
+};
+
+// A cluster of `blocks` blocks takes a row, each block a slice of it: one for many rows, up to eight for few.  Pass 1
+// reads the row for its sums, pass 2 reads it again (from L2: the rows in flight fit there) and writes the gradient.
+// Several blocks share an SM, so that one row's fixed costs - the list's dependent loads, the joins, the coefficients -
+// run beside other rows' sums.  The listed tokens enter the sums from the list, so that the sum over the rest costs a
+// byte of the bitmap per vector and never a difference of two large sums.
+//
+// What bounds it, apart from device memory: exponentials, one per element and pass.  exp(z - m) is the square of
+// exp((z - m) / 2), so at temperature 2 the hard part needs none of its own (kPower 2), at temperature 1 it is the
+// soft part's (kPower 0, also where there is no hard part); other temperatures pay for both (kPower -1).
+template <typename T, int kPower>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const DistillArgs a, const int blocks, const WaitLimit limit)
 {
-    constexpr int E = Vec<T>::kElems;
+    constexpr int E = Vec<T>::kElems, P = Pairs<T>::kCount;
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    __shared__ float scratch[32];
-    __shared__ Sums part[kStreamWarps];
-    float *p_s = reinterpret_cast<float *>(smem_raw);                  // [top] teacher's probability, 0 for a skipped entry
-    float *z_s = p_s + a.top;                                          // [top] student's logit there
-    int *i_s = reinterpret_cast<int *>(z_s + a.top);                   // [top] token, -1 for a skipped entry
-    uint32_t *bits = reinterpret_cast<uint32_t *>(i_s + a.top);        // listed tokens
-    const long long row = blockIdx.x;
-    const int tid = threadIdx.x;
+    __shared__ DistillShared sh;
+    Entry *list = reinterpret_cast<Entry *>(smem_raw);                                   // [top]
+    uint32_t *bits = reinterpret_cast<uint32_t *>(smem_raw + sizeof(Entry) * a.top);     // listed tokens
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const long long row = blockIdx.x / (unsigned)blocks;
+    const int rank = (int)(blockIdx.x % (unsigned)blocks);
     const float inv_t = a.inv_t, c = kLog2e * inv_t;
     const T *z = static_cast<const T *>(a.logits) + row * a.ld_logits;
     T *grad = a.grad ? static_cast<T *>(a.grad) + row * a.ld_grad : nullptr;
+    const RowCut<T> cut(z, a.vocab);
+    // This block's vectors, and the single elements that its first threads take: the head's with the first block, the
+    // tail's with the last.
+    const int per = (cut.vecs + blocks - 1) / blocks, q0 = min(rank * per, cut.vecs), q1 = min(q0 + per, cut.vecs);
+    const int heads = rank == 0 ? cut.head : 0, singles = heads + (rank == blocks - 1 ? cut.tail : 0);
+    const int single = tid < heads ? tid : cut.head + cut.vecs * E + tid - heads;        // for tid < singles
+    auto mine = [&](int j) {
+        return j < cut.head ? rank == 0 : j >= cut.head + cut.vecs * E ? rank == blocks - 1 : (j - cut.head) / E >= q0 && (j - cut.head) / E < q1;
+    };
+    auto listed_bits = [&](int j) { return bits[(j + cut.shift) >> 5] >> ((j + cut.shift) & 31); };
+
+    // Vectors go kBatch at a time, the next batch's loads in flight beside this one's arithmetic; the first batch of a
+    // pass is asked for before the fixed costs that come ahead of it.
+    const uint4 *vectors = reinterpret_cast<const uint4 *>(z + cut.head);
+    constexpr uint32_t kNone = sizeof(T) == 4 ? kMinusInfBits<T> : kMinusInfBits<T> * 0x10001u;
+    uint4 word[kBatch], ahead[kBatch];
+    auto fetch = [&](int q) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) ahead[k] = q + k * kThreads < q1 ? vectors[q + k * kThreads] : make_uint4(kNone, kNone, kNone, kNone);
+    };
+
     float w = a.weight ? a.weight[row] : 1.0f;
     if (a.grad_loss) w *= a.grad_loss[row];
-    const RowCut<T> cut(z, a.vocab);
-    const bool same = grad && (((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0);
-
+    fetch(q0 + tid);
     if (w == 0.0f) {        // nothing of the row is looked at
-        if (grad)
-            for (int j = tid; j < a.vocab; j += kStreamThreads) grad[j] = from_f32<T>(0.0f);
-        if (tid == 0) {
+        if (grad) {
+            const RowCut<T> g(grad, a.vocab);
+            const int gper = (g.vecs + blocks - 1) / blocks, g0 = min(rank * gper, g.vecs), g1 = min(g0 + gper, g.vecs);
+            for (int q = g0 + tid; q < g1; q += kThreads) reinterpret_cast<uint4 *>(grad + g.head)[q] = make_uint4(0, 0, 0, 0);
+            if (rank == 0 && tid < g.head + g.tail) grad[tid < g.head ? tid : g.vecs * E + tid] = from_f32<T>(0.0f);
+        }
+        if (tid == 0 && rank == 0) {
             if (a.loss) a.loss[row] = 0.0f;
             if (a.stats) reinterpret_cast<float4 *>(a.stats)[row] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
         return;
     }
+    if (tid == 0) {
+        sh.twice = 0;
+        sh.gave_up = 0;
+        if (blocks > 1) {
+            mbar_init(smem_addr(&sh.exchange), (uint32_t)blocks);
+            mbar_init_done();
+        }
+    }
 
-    // The teacher's list.
-    const int words = (a.vocab + E + 31) / 32;
-    for (int k = tid; k < words; k += kStreamThreads) bits[k] = 0;
-    float high = -INFINITY;
-    int any = 0;
-    for (int k = tid; k < a.top; k += kStreamThreads) {
+    // The list.
+    for (int k = tid; k < (a.vocab + E + 31) / 32; k += kThreads) bits[k] = 0;
+    for (int k = tid; k < a.top; k += kThreads) {
         const int i = a.index[row * a.top + k];
         const bool ok = i >= 0 && i < a.vocab;
-        const float t = to_f32(static_cast<const T *>(a.teacher)[row * a.top + k]);
-        i_s[k] = ok ? i : -1;
-        p_s[k] = t;
-        z_s[k] = ok ? to_f32(z[i]) : 0.0f;
-        if (ok) {
-            high = fmaxf(high, t);
-            any = 1;
-        }
-    }
-    any = __syncthreads_or(any);
-    int twice = 0;           // a token is listed more than once
-    for (int k = tid; k < a.top; k += kStreamThreads)
-        if (i_s[k] >= 0) {
-            const uint32_t bit = 1u << ((i_s[k] + cut.shift) & 31);
-            twice |= (atomicOr(&bits[(i_s[k] + cut.shift) >> 5], bit) & bit) != 0;
-        }
-    twice = __syncthreads_or(twice);
-    float log_norm;          // log of the teacher's normaliser at temperature T
-    if (a.lse) {
-        log_norm = a.lse[row];
-    } else {
-        high = base_of(block_max<kStreamWarps>(high, scratch));
-        float sum = 0.0f;
-        for (int k = tid; k < a.top; k += kStreamThreads)
-            if (i_s[k] >= 0) sum += ex2((p_s[k] - high) * c);
-        sum = block_sum<kStreamWarps>(sum, scratch);
-        if (sum == 0.0f) any = 0;            // a list of -inf says nothing
-        log_norm = any ? logf(sum) + high * inv_t : 0.0f;
-    }
-    float mass = 0.0f, soft = 0.0f;      // sum p; sum p (log p - (z_k - m) / T) without the student's part yet
-    for (int k = tid; k < a.top; k += kStreamThreads) {
-        const float log_p = p_s[k] * inv_t - log_norm;
-        const float p = i_s[k] >= 0 ? ex2(log_p * kLog2e) : 0.0f;
-        p_s[k] = p;
-        mass += p;
-        if (p > 0.0f) soft += p * log_p;
-        else if (p != p) soft += p;
-    }
-    mass = block_sum<kStreamWarps>(mass, scratch);
-    const float p_rest = a.lse ? fmaxf(0.0f, 1.0f - mass) : 0.0f;
-
-    // The student's sums.
-    Sums t{-INFINITY, 0.0f, 0.0f, 0.0f};
-    if (a.stats_in) {
-        const float4 s4 = reinterpret_cast<const float4 *>(a.stats_in)[row];
-        t = Sums{s4.x, s4.y, s4.z, s4.w};
-    } else {
-        auto take = [&](const float *v, uint32_t listed, int n) {
-            float vm = v[0];
-            for (int k = 1; k < n; ++k) vm = fmaxf(vm, v[k]);
-            if (vm > t.m) {
-                const float f = ex2((t.m - vm) * c);
-                t.s *= f;
-                t.r *= f;
-                t.s1 *= ex2((t.m - vm) * kLog2e);
-                t.m = vm;
-            }
-            const float b = base_of(t.m);
-            for (int k = 0; k < n; ++k) {
-                const float e = ex2((v[k] - b) * c);
-                t.s += e;
-                if (!(listed >> k & 1)) t.r += e;
-                t.s1 += ex2((v[k] - b) * kLog2e);
-            }
-        };
-        for (int q = tid; q < cut.vecs; q += kStreamThreads) {
-            const int j = cut.head + q * E;
-            float v[E];
-            Vec<T>::unpack(*reinterpret_cast<const uint4 *>(z + j), v);
-            take(v, bits[(j + cut.shift) >> 5] >> ((j + cut.shift) & 31), E);
-        }
-        for (int x = tid; x < cut.head + cut.tail; x += kStreamThreads) {
-            const int j = x < cut.head ? x : cut.vecs * E + x;
-            const float v = to_f32(z[j]);
-            take(&v, bits[(j + cut.shift) >> 5] >> ((j + cut.shift) & 31), 1);
-        }
-        t = shuffle_join(t, c);
-        if ((tid & 31) == 0) part[tid >> 5] = t;
-        __syncthreads();
-        t = part[0];
-        for (int k = 1; k < kStreamWarps; ++k) t = join(t, part[k], c);
-        t.m = base_of(t.m);
+        list[k] = Entry{ok ? i : -1, ok ? to_f32(z[i]) : 0.0f, to_f32(static_cast<const T *>(a.teacher)[row * a.top + k])};
     }
     const int label = a.labels ? a.labels[row] : -1;
     const bool hard = label >= 0 && label < a.vocab;
+    const float z_label = hard ? to_f32(z[label]) : 0.0f;
+    __syncthreads();
+    // From here on other blocks may replace their slices of the row by gradients, once they have waited for this.
+    if (blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+
+    Sums t{-INFINITY, 0.0f, 0.0f, 0.0f};
+    for (int k = tid; k < a.top; k += kThreads) {
+        const int i = list[k].token;
+        if (i < 0) continue;
+        const uint32_t bit = 1u << ((i + cut.shift) & 31);
+        if (atomicOr(&bits[(i + cut.shift) >> 5], bit) & bit) {
+            sh.twice = 1;
+        } else if (!a.stats_in && mine(i)) {       // the listed tokens' share of the sums, each token once
+            const float x = list[k].z, one = x == -INFINITY ? 0.0f : 1.0f + 0.0f * x;      // NaN for +inf and NaN
+            t = join(t, Sums{x, one, one, 0.0f}, c);
+        }
+    }
+    __syncthreads();
+    if (warp == kWarps - 1) {          // the teacher's probabilities, by one warp beside the others' sums
+        float high = -INFINITY;
+        bool some = false;
+        for (int k = lane; k < a.top; k += 32)
+            if (list[k].token >= 0) {
+                some = true;
+                high = fmaxf(high, list[k].p);
+            }
+        int any = __any_sync(0xffffffffu, some);
+        float log_norm = a.lse ? a.lse[row] : 0.0f;
+        if (!a.lse) {
+            high = base_of(warp_max(high));
+            float sum = 0.0f;
+            for (int k = lane; k < a.top; k += 32)
+                if (list[k].token >= 0) sum += ex2((list[k].p - high) * c);
+            sum = warp_sum(sum);
+            if (sum == 0.0f) any = 0;            // a list of -inf says nothing
+            log_norm = any ? logf(sum) + high * inv_t : 0.0f;
+        }
+        float mass = 0.0f, soft = 0.0f;
+        for (int k = lane; k < a.top; k += 32) {
+            const float log_p = list[k].p * inv_t - log_norm;
+            const float p = list[k].token >= 0 && any ? ex2(log_p * kLog2e) : 0.0f;
+            list[k].p = p;
+            mass += p;
+            if (p != 0.0f) soft += p * log_p;
+        }
+        mass = warp_sum(mass);
+        soft = warp_sum(soft);
+        if (lane == 0) {
+            sh.mass = mass;
+            sh.soft = soft;
+            sh.any = any;
+        }
+    }
+
+    // The student's sums.
+    if (a.stats_in) {
+        const float4 s4 = reinterpret_cast<const float4 *>(a.stats_in)[row];
+        t = Sums{s4.x, s4.y, s4.z, s4.w};
+        __syncthreads();
+    } else {
+        uint64_t minus_m = pair(-base_of(t.m), -base_of(t.m)), s2 = pair(0.0f, 0.0f), f2 = s2;
+        float m = t.m;
+        const uint64_t c2 = pair(c, c), l2 = pair(kLog2e, kLog2e);
+        // The base need not be the maximum itself: powers up to 2^40 above it lose nothing in binary32, and the sums are
+        // rebased for a logit further above alone (else nearly every vector would, for one lane or other).
+        const float slack = 40.0f / fmaxf(c, kLog2e);
+        auto rebase = [&](float vm) {
+            if (vm > m + slack) {
+                const float f = ex2((m - vm) * c), f1 = ex2((m - vm) * kLog2e);
+                s2 = mul2(s2, pair(f, f));
+                f2 = mul2(f2, pair(f1, f1));
+                t.s *= f;
+                t.s1 *= f1;
+                m = vm;
+                minus_m = pair(-m, -m);
+            }
+        };
+        auto take = [&](const uint4 &word) {
+            uint64_t x[P];
+            Pairs<T>::unpack(word, x);
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                const uint64_t d = add2(x[k], minus_m), e = ex2_2(mul2(d, c2));
+                s2 = add2(s2, e);
+                if (kPower == 2) f2 = fma2(e, e, f2);
+                if (kPower == -1) f2 = add2(f2, ex2_2(mul2(d, l2)));
+            }
+        };
+        const uint8_t *vector_bits = reinterpret_cast<const uint8_t *>(bits) ;
+        const int first_bit = cut.head + cut.shift;          // a multiple of E
+        auto without_listed = [&](uint4 word, int q) {       // listed elements as -inf
+            uint32_t in = E == 8 ? vector_bits[(first_bit >> 3) + q] : vector_bits[(first_bit + q * E) >> 3] >> ((first_bit + q * E) & 7) & 15u;
+            if (in) {
+                uint32_t *x = &word.x;
+#pragma unroll
+                for (int k = 0; k < E; ++k)
+                    if (in >> k & 1) {
+                        if (E == 4) x[k] = kNone;
+                        else x[k >> 1] = k & 1 ? (x[k >> 1] & 0xFFFFu) | (kNone & 0xFFFF0000u) : (x[k >> 1] & 0xFFFF0000u) | (kNone & 0xFFFFu);
+                    }
+            }
+            return word;
+        };
+        for (int q = q0 + tid; q < q1; q += kBatch * kThreads) {
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) word[k] = ahead[k];
+            fetch(q + kBatch * kThreads);
+            float vm = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (q + k * kThreads < q1) word[k] = without_listed(word[k], q + k * kThreads);
+                vm = fmaxf(vm, Pairs<T>::largest(word[k]));
+            }
+            rebase(vm);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                if (k == 0 || q + k * kThreads < q1) take(word[k]);
+        }
+        if (tid < singles && !(listed_bits(single) & 1)) {
+            const float x = to_f32(z[single]), b = base_of(fmaxf(m, x));
+            const float f = x > m ? ex2((m - b) * c) : 1.0f, f1 = x > m ? ex2((m - b) * kLog2e) : 1.0f;
+            s2 = add2(mul2(s2, pair(f, f)), pair(ex2((x - b) * c), 0.0f));
+            f2 = add2(mul2(f2, pair(f1, f1)), pair(ex2((x - b) * kLog2e), 0.0f));
+            t.s *= f;
+            t.s1 *= f1;
+            m = fmaxf(m, x);
+        }
+        if (grad) fetch(q0 + tid);
+        float lo, hi;
+        unpair(s2, lo, hi);
+        t.m = m;
+        t.r = lo + hi;
+        t.s += t.r;
+        unpair(f2, lo, hi);
+        t.s1 = kPower == 0 ? t.s : t.s1 + (lo + hi);
+        t = warp_join(t, c);
+        if (lane == 0) sh.part[warp] = t;
+        __syncthreads();
+        t = warp_join(lane < kWarps ? sh.part[lane] : Sums{-INFINITY, 0.0f, 0.0f, 0.0f}, c);
+        if (blocks > 1) {      // every block tells every block
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            const uint32_t bar = smem_addr(&sh.exchange);
+            if (warp == 0 && lane < blocks) {
+                uint32_t remote;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_addr(&sh.theirs[rank])), "r"(lane));
+                asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(remote), "f"(t.m), "f"(t.s), "f"(t.s1), "f"(t.r)
+                             : "memory");
+                mbar_arrive_at(bar, (uint32_t)lane);
+            }
+            mbar_wait<true>(bar, 0, &sh.gave_up, limit);
+            t = warp_join(lane < blocks ? sh.theirs[lane] : Sums{-INFINITY, 0.0f, 0.0f, 0.0f}, c);
+        }
+        t.m = base_of(t.m);
+        if (a.stats && tid == 0 && rank == 0) reinterpret_cast<float4 *>(a.stats)[row] = make_float4(t.m, t.s, t.s1, t.r);
+    }
+    if (blocks > 1) {          // nobody leaves before the others are done with its memory
+        if (a.stats_in) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    }
+
+    const bool any = sh.any;
     const bool empty = t.s == 0.0f;      // every token masked out
+    const float mass = sh.mass, p_rest = a.lse ? fmaxf(0.0f, 1.0f - mass) : 0.0f;
     const bool rest = p_rest > 0.0f && t.r > kLeastRest * t.s;
-    const float log_s = logf(t.s);
-    if (a.stats && tid == 0) reinterpret_cast<float4 *>(a.stats)[row] = make_float4(t.m, t.s, t.s1, t.r);
-    if (a.loss) {
-        for (int k = tid; k < a.top; k += kStreamThreads)
-            if (p_s[k] > 0.0f) soft -= p_s[k] * ((z_s[k] - t.m) * inv_t - log_s);
-        soft = block_sum<kStreamWarps>(soft, scratch);
+    if (a.loss && rank == 0 && warp == 0) {
+        const float log_s = logf(t.s);
+        float soft = 0.0f;
+        for (int k = lane; k < a.top; k += 32)
+            if (list[k].p != 0.0f) soft -= list[k].p * ((list[k].z - t.m) * inv_t - log_s);
+        soft = warp_sum(soft) + sh.soft;
         if (rest) soft += p_rest * (logf(p_rest) - (logf(t.r) - log_s));
         float loss = any ? a.soft_weight * a.temperature * a.temperature * soft : 0.0f;
-        if (hard) loss += a.hard_weight * (logf(t.s1) - (to_f32(z[label]) - t.m));
+        if (hard) loss += a.hard_weight * (logf(t.s1) - (z_label - t.m));
         if (t.s != t.s) loss = t.s;
-        if (tid == 0) a.loss[row] = empty ? 0.0f : w * loss;
+        if (lane == 0) a.loss[row] = empty ? 0.0f : w * loss;
     }
-    if (!grad) return;
-    __syncthreads();
-    const float z_label = hard ? to_f32(z[label]) : 0.0f;
-    const float c0 = any ? w * a.soft_weight * a.temperature : 0.0f;
-    const float ca = empty ? 0.0f : c0 * (a.lse ? mass + p_rest : 1.0f) / t.s;
-    const float cu = rest && !empty ? ca - c0 * p_rest / t.r : ca;
-    const float ch = hard ? w * a.hard_weight : 0.0f;
-    const float cb = empty ? 0.0f : ch / t.s1;
-    const float nan = t.s != t.s ? t.s : 0.0f;     // a NaN row is NaN throughout
-    __syncthreads();                               // z_label has been read before grad may replace it
-    for (int q = tid; q < cut.vecs; q += kStreamThreads) {
-        const int j = cut.head + q * E;
-        float v[E];
-        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(z + j), v);
+    if (grad) {
+        const float c0 = any ? w * a.soft_weight * a.temperature : 0.0f;
+        const float ca = empty ? 0.0f : c0 * (a.lse ? mass + p_rest : 1.0f) / t.s;
+        const float cu = rest && !empty ? ca - c0 * p_rest / t.r : ca;
+        const float ch = hard ? w * a.hard_weight : 0.0f;
+        const float cb = empty ? 0.0f : ch / t.s1;
+        const uint64_t minus_m = pair(-t.m, -t.m), c2 = pair(c, c), l2 = pair(kLog2e, kLog2e);
+        // temperature 1, or no hard part at all: the two exponentials are one
+        const float cu_all = kPower == 0 ? cu + cb : cu;
+        const uint64_t cu2 = pair(cu_all, cu_all), cb2 = pair(cb, cb);
+        const bool same = ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0;
+        for (int q = q0 + tid; q < q1; q += kBatch * kThreads) {
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-            const float d = v[k] - t.m;
-            v[k] = cu * ex2(d * c) + (hard ? cb * ex2(d * kLog2e) : 0.0f) + nan;
-        }
-        if (same) {
-            *reinterpret_cast<uint4 *>(grad + j) = Vec<T>::pack(v);
-        } else {
+            for (int k = 0; k < kBatch; ++k) word[k] = ahead[k];
+            fetch(q + kBatch * kThreads);
 #pragma unroll
-            for (int k = 0; k < E; ++k) grad[j + k] = from_f32<T>(v[k]);
+            for (int h = 0; h < kBatch; ++h) {
+                if (q + h * kThreads >= q1) break;
+                uint64_t x[P];
+                Pairs<T>::unpack(word[h], x);
+#pragma unroll
+                for (int k = 0; k < P; ++k) {
+                    const uint64_t d = add2(x[k], minus_m), e = ex2_2(mul2(d, c2));
+                    if (kPower == 0) x[k] = mul2(cu2, e);
+                    if (kPower == 2) x[k] = mul2(e, fma2(cb2, e, cu2));
+                    if (kPower == -1) x[k] = fma2(cb2, ex2_2(mul2(d, l2)), mul2(cu2, e));
+                }
+                if (same) {
+                    __stcs(reinterpret_cast<uint4 *>(grad + cut.head) + q + h * kThreads, Pairs<T>::pack(x));
+                } else {
+                    T *g = grad + cut.head + (q + h * kThreads) * E;
+#pragma unroll
+                    for (int k = 0; k < P; ++k) {
+                        float lo, hi;
+                        unpair(x[k], lo, hi);
+                        g[2 * k] = from_f32<T>(lo);
+                        g[2 * k + 1] = from_f32<T>(hi);
+                    }
+                }
+            }
+        }
+        if (tid < singles) {
+            const float d = to_f32(z[single]) - t.m;
+            grad[single] = from_f32<T>(cu * ex2(d * c) + cb * ex2(d * kLog2e));
+        }
+        __syncthreads();
+        // Listed tokens and the label, in binary32 from their own logits, over what has been stored there.
+        const bool twice = sh.twice;
+        for (int k = tid; k < a.top; k += kThreads) {
+            const int i = list[k].token;
+            if (i < 0 || !mine(i)) continue;
+            float p = list[k].p;
+            if (twice) {       // all its entries together, in the same order for each of them
+                p = 0.0f;
+                for (int o = 0; o < a.top; ++o) p += list[o].token == i ? list[o].p : 0.0f;
+            }
+            const float d = list[k].z - t.m;
+            float g = ca * ex2(d * c) - c0 * p + cb * ex2(d * kLog2e);
+            if (i == label) g -= ch;
+            grad[i] = from_f32<T>(empty ? 0.0f : g);
+        }
+        if (hard && tid == 0 && mine(label) && !(listed_bits(label) & 1)) {
+            const float d = z_label - t.m;
+            grad[label] = from_f32<T>(empty ? 0.0f : cu * ex2(d * c) + cb * ex2(d * kLog2e) - ch);
         }
     }
-    for (int x = tid; x < cut.head + cut.tail; x += kStreamThreads) {
-        const int j = x < cut.head ? x : cut.vecs * E + x;
-        const float d = to_f32(z[j]) - t.m;
-        grad[j] = from_f32<T>(cu * ex2(d * c) + (hard ? cb * ex2(d * kLog2e) : 0.0f) + nan);
-    }
-    __syncthreads();
-    // Listed tokens and the label, in binary32 from their own logits, over what the loops above stored there.
-    for (int k = tid; k < a.top; k += kStreamThreads) {
-        const int i = i_s[k];
-        if (i < 0) continue;
-        const float d = z_s[k] - t.m;
-        float p = p_s[k];
-        if (twice) {         // all its entries together, in the same order for each of them
-            p = 0.0f;
-            for (int o = 0; o < a.top; ++o) p += i_s[o] == i ? p_s[o] : 0.0f;
-        }
-        float v = ca * ex2(d * c) - c0 * p + (hard ? cb * ex2(d * kLog2e) : 0.0f) + nan;
-        if (i == label) v -= ch;
-        grad[i] = from_f32<T>(empty ? 0.0f : v);
-    }
-    if (hard && tid == 0 && !(bits[(label + cut.shift) >> 5] >> ((label + cut.shift) & 31) & 1)) {
-        const float d = z_label - t.m;
-        grad[label] = from_f32<T>(empty ? 0.0f : cu * ex2(d * c) + cb * ex2(d * kLog2e) - ch + nan);
-    }
+    if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <typename T, int kPower>
+void launch_kernel(const DistillArgs &a, int blocks, const WaitLimit &wait_limit, cudaStream_t s)
+{
+    static SmemLimit limit;
+    auto kernel = distill_kernel<T, kPower>;
+    if (limit.ensure(kernel, (int)(kMaxTop * sizeof(Entry) + kMaxVocab / 8 + 64)) != cudaSuccess) return;     // the caller reports it
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(a.rows * blocks));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = sizeof(Entry) * (size_t)a.top + (size_t)(a.vocab + Vec<T>::kElems + 31) / 32 * 4;
+    cfg.stream = s;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim = {(unsigned)blocks, 1, 1};
+    cfg.attrs = &at;
+    cfg.numAttrs = blocks > 1;
+    cudaLaunchKernelEx(&cfg, kernel, a, blocks, wait_limit);
 }
 
 zoa_status launch(const char *me, const zoa_distill_args *x, const float *stats_in, const float *grad_loss, float *loss, float *stats,
@@ -325,6 +566,7 @@ zoa_status launch(const char *me, const zoa_distill_args *x, const float *stats_
     if (!aligned16(stats) || !aligned16(stats_in)) return ops_fail(ZOA_ERR_ARG, "%s: stats must be 16-byte aligned", me);
     if (grad == x->logits && ld_grad != x->ld_logits)
         return ops_fail(ZOA_ERR_ARG, "%s: a gradient that replaces the logits has their ld", me);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
     DistillArgs a{};
     a.logits = x->logits;
     a.index = x->index;
@@ -346,12 +588,18 @@ zoa_status launch(const char *me, const zoa_distill_args *x, const float *stats_
     a.inv_t = 1.0f / x->temperature;
     a.soft_weight = x->soft_weight;
     a.hard_weight = x->hard_weight;
+    const int sms = ops_sm_count();
+    WaitLimit wait_limit{ops_error_word(), ops_wait_limit_ns()};
+    if (sms < 1 || !wait_limit.error_word) return ops_fail(ZOA_ERR_CUDA, "%s: no usable current device", me);
+    // Blocks for a row: more while there are SMs without one and a slice stays above 4 KB.
+    int blocks = 1;
+    while (blocks < kMaxCluster && a.rows * blocks * 2 <= 2 * sms && (size_t)a.vocab * e / (blocks * 2) >= 4096) blocks *= 2;
+    if (a.rows * blocks > 0x7FFFFFFFll) return ops_fail(ZOA_ERR_ARG, "%s: at most 2^31 - 1 rows", me);
     with_type(x->dtype, [&](auto t) {
         using T = decltype(t);
-        const int smem = a.top * 12 + (a.vocab + Vec<T>::kElems + 31) / 32 * 4;
-        static SmemLimit limit;
-        if (limit.ensure(distill_stream_kernel<T>, (int)(kMaxTop * 12 + kMaxVocab / 8 + 64)) != cudaSuccess) return;
-        distill_stream_kernel<T><<<(unsigned)a.rows, kStreamThreads, smem, static_cast<cudaStream_t>(stream)>>>(a);
+        if (a.temperature == 1.0f || !a.labels) launch_kernel<T, 0>(a, blocks, wait_limit, s);
+        else if (a.temperature == 2.0f) launch_kernel<T, 2>(a, blocks, wait_limit, s);
+        else launch_kernel<T, -1>(a, blocks, wait_limit, s);
     });
     return ops_launched(me);
 }

@@ -1,63 +1,10 @@
 // Products of 4-bit microscaled matrices on the tensor cores: C[i, j] = sum_k A[i, k] B[j, k], both operands in the
 // tiles of zoa_mx4.cuh, sums in binary32.
+#include "zoa_async.cuh"
 #include "zoa_mx4.cuh"
 
 namespace zoa {
 namespace {
-
-// ---- barriers and copies, every wait bounded ----------------------------------------------------------------
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ unsigned long long timer_ns()
-{
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-struct WaitLimit {
-    int *error_word;            // set when a wait ran out
-    unsigned long long ns;
-};
-// False if the block has given up or the limit ran out (both flags are then set).
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, const WaitLimit &limit)
-{
-    if (mbar_try(bar, parity)) return true;
-    const unsigned long long start = timer_ns();
-    for (unsigned it = 1;; ++it) {
-        if (mbar_try(bar, parity)) return true;
-        if (*gave_up) return false;
-        if ((it & 63u) == 0 && timer_ns() - start > limit.ns) {
-            *gave_up = 1;
-            atomicExch(limit.error_word, 1);
-            return false;
-        }
-    }
-}
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
-}
 
 // ---- tensor core ------------------------------------------------------------------------------------------
 // Shared-memory operand descriptors.  Codes: K-major, 128-byte swizzle, 8-row groups 1024 bytes apart.  Scales: no
@@ -215,10 +162,8 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
     __syncwarp();
     const bool finished = mbar_wait(smem_addr(&sh->done), 0, gave_up, g.limit);
     if (threadIdx.x == 0 && *gave_up) {      // copies in flight land before the block's shared memory is released
-        for (int q = issued > kStages ? issued - kStages : 0; q < issued; ++q) {
-            const unsigned long long start = timer_ns();
-            while (!mbar_try(smem_addr(&sh->full[q % kStages]), (uint32_t)(q / kStages & 1)) && timer_ns() - start < g.limit.ns) {}
-        }
+        for (int q = issued > kStages ? issued - kStages : 0; q < issued; ++q)
+            mbar_drain(smem_addr(&sh->full[q % kStages]), (uint32_t)(q / kStages & 1), g.limit);
     }
     if (warp >= 2 && finished && !*gave_up) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -304,4 +249,29 @@ extern "C" zoa_status zoa_mx4_linear(const void *x, int dtype, size_t m, size_t 
     if (m && n && k && zoa_mx4_linear_work(m, n, k) && !work) return ops_fail(ZOA_ERR_ARG, "zoa_mx4_linear: work is NULL");
     const zoa_status st = zoa_mx4_quantize(x, dtype, m, k, ldx, work, nullptr, stream);
     return st != ZOA_OK ? st : zoa_mx4_matmul(work, b, m, n, k, out, dtype, ld, stream);
+}
+
+extern "C" zoa_status zoa_mx4_linear_forward(const void *x, int x_type, size_t ldx, const void *w, int w_type, size_t ldw, size_t m,
+                                             size_t n, size_t k, void *y, size_t ldy, void *xt, void *wt, void *work, void *stream)
+{
+    const char *me = "zoa_mx4_linear_forward";
+    if (m && n && k && (!xt || !wt || !work)) return ops_fail(ZOA_ERR_ARG, "%s: a NULL pointer", me);
+    void *wq = static_cast<unsigned char *>(work) + zoa_mx4_size(m, k);
+    zoa_status st = zoa_mx4_quantize(x, x_type, m, k, ldx, work, xt, stream);
+    if (st == ZOA_OK) st = zoa_mx4_quantize(w, w_type, n, k, ldw, wq, wt, stream);
+    return st != ZOA_OK ? st : zoa_mx4_matmul(work, wq, m, n, k, y, x_type, ldy, stream);
+}
+
+extern "C" zoa_status zoa_mx4_linear_backward(const void *dy, int dy_type, size_t ld_dy, size_t m, size_t n, size_t k, const void *xt,
+                                              const void *wt, void *dx, int dx_type, size_t ld_dx, void *dw, int dw_type, size_t ld_dw,
+                                              void *work, void *stream)
+{
+    const char *me = "zoa_mx4_linear_backward";
+    if (!dx && !dw) return ops_fail(ZOA_ERR_ARG, "%s: neither dx nor dw is asked for", me);
+    if (m && n && !work) return ops_fail(ZOA_ERR_ARG, "%s: work is NULL", me);
+    void *dyt = static_cast<unsigned char *>(work) + zoa_mx4_size(m, n);
+    zoa_status st = zoa_mx4_quantize(dy, dy_type, m, n, ld_dy, dx ? work : nullptr, dw ? dyt : nullptr, stream);
+    if (st == ZOA_OK && dx) st = zoa_mx4_matmul(work, wt, m, k, n, dx, dx_type, ld_dx, stream);
+    if (st == ZOA_OK && dw) st = zoa_mx4_matmul(dyt, xt, n, k, m, dw, dw_type, ld_dw, stream);
+    return st;
 }

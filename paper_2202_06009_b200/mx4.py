@@ -1,38 +1,63 @@
 """4-bit microscaled matrices and the linear layer on them (include/zoa.h: zoa_mx4_*), on torch tensors.
 
-Argument checks and marshalling only; the arithmetic runs in the library's kernels, on the current stream.
+Argument checks and marshalling only; the arithmetic runs in the library's kernels, on the current stream.  A call on
+few tokens lasts as long as its Python: the checks are kept short, and calls go to the library without a layer between.
 """
 import torch
 
 from . import binding as B
 
+_lib = B.lib
 _TYPES = {torch.float32: B.F32, torch.float16: B.F16, torch.bfloat16: B.BF16}
+_current_device = torch.cuda.current_device
+_raw_stream = torch._C._cuda_getCurrentRawStream      # of a device's current stream, without the Stream object around it
+_TILE_ROWS, _TILE_COLS, _TILE_BYTES = 128, 256, B.zoa_mx4_size(1, 1)
+_MAX_SIDE = 1 << 30
 
 
 def _matrix(x, what):
-    """Type number and row distance of a 2-D CUDA tensor whose rows are contiguous."""
+    """(type number, rows, cols, row distance) of a 2-D CUDA tensor whose rows are contiguous."""
     code = _TYPES.get(x.dtype)
     if code is None:
         raise ValueError(f"{what} must be float32, float16 or bfloat16, not {x.dtype}")
     if x.dim() != 2 or not x.is_cuda:
         raise ValueError(f"{what} must be a 2-D CUDA tensor")
-    ld, step = x.stride()
     rows, cols = x.shape
-    if (step != 1 and cols > 1) or (ld < cols and rows > 1):
-        raise ValueError(f"the rows of {what} must be contiguous and must not overlap")
-    return code, max(ld, cols)
+    ld, step = x.stride()
+    if ld < cols or step != 1:
+        if (step != 1 and cols > 1) or (ld < cols and rows > 1):
+            raise ValueError(f"the rows of {what} must be contiguous and must not overlap")
+        ld = max(ld, cols)
+    return code, rows, cols, ld
 
 
-def _result(out, rows, cols, dtype, like, what="out"):
-    if out is None:
-        out = torch.empty((rows, cols), dtype=dtype, device=like)
-    elif out.shape != (rows, cols) or out.dtype != dtype or out.device != like:
-        raise ValueError(f"{what} must be a {dtype} tensor of shape ({rows}, {cols}) on {like}")
-    return out
+def _check_result(out, rows, cols, dtype, device, what="out"):
+    if out.shape != (rows, cols) or out.dtype != dtype or out.device != device:
+        raise ValueError(f"{what} must be a {dtype} tensor of shape ({rows}, {cols}) on {device}")
+    return _matrix(out, what)[3]
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+def _call(fn, device, *args):
+    """fn(*args, stream) with `device` current, on its current stream."""
+    index = device.index
+    if index == _current_device():
+        status = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    if status:
+        B._check_ops(status)
+
+
+def _size(rows, cols):
+    """zoa_mx4_size."""
+    if rows > _MAX_SIDE or cols > _MAX_SIDE:
+        raise ValueError("a side of an Mx4 is at most 2^30")
+    return -(-rows // _TILE_ROWS) * -(-cols // _TILE_COLS) * _TILE_BYTES
+
+
+def _bytes(n, device):
+    return torch.empty(n, dtype=torch.uint8, device=device)
 
 
 class Mx4:
@@ -42,9 +67,9 @@ class Mx4:
     __slots__ = ("data", "rows", "cols")
 
     def __init__(self, rows, cols, device="cuda", data=None):
-        size = B.zoa_mx4_size(rows, cols)
+        size = _size(rows, cols)
         if data is None:
-            data = torch.empty(size, dtype=torch.uint8, device=device)
+            data = _bytes(size, device)
         elif data.dtype != torch.uint8 or not data.is_cuda or not data.is_contiguous() or data.numel() != size or data.data_ptr() % 16:
             raise ValueError(f"data must be a contiguous, 16-byte aligned uint8 CUDA tensor of {size} bytes")
         self.data, self.rows, self.cols = data, rows, cols
@@ -59,10 +84,15 @@ class Mx4:
 
     def dequantize(self, dtype=torch.bfloat16, out=None):
         """The values it stands for (exact in float32 and bfloat16)."""
-        out = _result(out, self.rows, self.cols, dtype, self.data.device)
-        code, ld = _matrix(out, "out")
-        with torch.cuda.device(self.data.device):
-            B.zoa_mx4_dequantize(self.data.data_ptr(), self.rows, self.cols, out.data_ptr(), code, ld, _stream(self.data.device))
+        data, rows, cols = self.data, self.rows, self.cols
+        device = data.device
+        if out is None:
+            if dtype not in _TYPES:
+                raise ValueError(f"dtype must be float32, float16 or bfloat16, not {dtype}")
+            out, ld = torch.empty((rows, cols), dtype=dtype, device=device), cols
+        else:
+            ld = _check_result(out, rows, cols, dtype, device)
+        _call(_lib.zoa_mx4_dequantize, device, data.data_ptr(), rows, cols, out.data_ptr(), _TYPES[dtype], ld)
         return out
 
 
@@ -76,73 +106,103 @@ def _form(out, rows, cols, device, what):
 
 def mx4_quantize(x, out=None):
     """x [rows, cols] rounded along its rows."""
-    code, ld = _matrix(x, "x")
-    rows, cols = x.shape
-    out = _form(out, rows, cols, x.device, "out")
-    with torch.cuda.device(x.device):
-        B.zoa_mx4_quantize(x.data_ptr(), code, rows, cols, ld, out.data.data_ptr(), None, _stream(x.device))
+    code, rows, cols, ld = _matrix(x, "x")
+    device = x.device
+    out = _form(out, rows, cols, device, "out")
+    _call(_lib.zoa_mx4_quantize, device, x.data_ptr(), code, rows, cols, ld, out.data.data_ptr(), None)
     return out
 
 
 def mx4_quantize_both(x, out=None, out_t=None):
     """x rounded along its rows, and its transpose rounded along its rows (x's columns), from one read."""
-    code, ld = _matrix(x, "x")
-    rows, cols = x.shape
-    out = _form(out, rows, cols, x.device, "out")
-    out_t = _form(out_t, cols, rows, x.device, "out_t")
-    with torch.cuda.device(x.device):
-        B.zoa_mx4_quantize(x.data_ptr(), code, rows, cols, ld, out.data.data_ptr(), out_t.data.data_ptr(), _stream(x.device))
+    code, rows, cols, ld = _matrix(x, "x")
+    device = x.device
+    out = _form(out, rows, cols, device, "out")
+    out_t = _form(out_t, cols, rows, device, "out_t")
+    _call(_lib.zoa_mx4_quantize, device, x.data_ptr(), code, rows, cols, ld, out.data.data_ptr(), out_t.data.data_ptr())
     return out, out_t
 
 
 def mx4_matmul(a, b, dtype=torch.bfloat16, out=None):
     """a [m, k] times b [n, k] transposed, both Mx4: [m, n] of `dtype`."""
-    if a.cols != b.cols:
+    m, n, k, device = a.rows, b.rows, a.cols, a.data.device
+    if k != b.cols:
         raise ValueError(f"a is {a.shape}, b is {b.shape}: their columns must agree")
-    if a.device != b.device:
+    if b.data.device != device:
         raise ValueError("a and b must be on the same device")
-    out = _result(out, a.rows, b.rows, dtype, a.device)
-    code, ld = _matrix(out, "out")
-    with torch.cuda.device(a.device):
-        B.zoa_mx4_matmul(a.data.data_ptr(), b.data.data_ptr(), a.rows, b.rows, a.cols, out.data_ptr(), code, ld, _stream(a.device))
+    if out is None:
+        if dtype not in _TYPES:
+            raise ValueError(f"dtype must be float32, float16 or bfloat16, not {dtype}")
+        out, ld = torch.empty((m, n), dtype=dtype, device=device), n
+    else:
+        ld = _check_result(out, m, n, dtype, device)
+    _call(_lib.zoa_mx4_matmul, device, a.data.data_ptr(), b.data.data_ptr(), m, n, k, out.data_ptr(), _TYPES[dtype], ld)
     return out
 
 
 def mx4_linear(x, w, out=None):
     """Q(x) w^T for activations x [tokens, in] and a weight w, Mx4 [out, in]; the result has x's type."""
-    code, ld = _matrix(x, "x")
-    m, k = x.shape
+    code, m, k, ldx = _matrix(x, "x")
+    device, n = x.device, w.rows
     if k != w.cols:
         raise ValueError(f"x is {tuple(x.shape)}, w is {w.shape}: their columns must agree")
-    if w.device != x.device:
+    if w.data.device != device:
         raise ValueError("x and w must be on the same device")
-    n = w.rows
-    out = _result(out, m, n, x.dtype, x.device)
-    _, ld_out = _matrix(out, "out")
-    size = B.zoa_mx4_linear_work(m, n, k)
-    work = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
-    with torch.cuda.device(x.device):
-        B.zoa_mx4_linear(x.data_ptr(), code, m, k, ld, w.data.data_ptr(), n, out.data_ptr(), ld_out,
-                         work.data_ptr() if size else None, _stream(x.device))
+    if out is None:
+        out, ld = torch.empty((m, n), dtype=x.dtype, device=device), n
+    else:
+        ld = _check_result(out, m, n, x.dtype, device)
+    size = _lib.zoa_mx4_linear_work(m, n, k)
+    work = _bytes(size, device) if size else None
+    _call(_lib.zoa_mx4_linear, device, x.data_ptr(), code, m, k, ldx, w.data.data_ptr(), n, out.data_ptr(), ld,
+          work.data_ptr() if size else None)
     return out
+
+
+class Mx4LinearSaved:
+    """What mx4_linear_backward needs of a forward step: x^T and w^T rounded along their rows, in one buffer."""
+    __slots__ = ("data", "m", "n", "k", "x_dtype", "w_dtype")
+
+    def __init__(self, data, m, n, k, x_dtype, w_dtype):
+        self.data, self.m, self.n, self.k, self.x_dtype, self.w_dtype = data, m, n, k, x_dtype, w_dtype
 
 
 def mx4_linear_forward(x, w):
     """Training form: y = Q(x) Q(w)^T from real x [tokens, in] and w [out, in], and what mx4_linear_backward needs
     (x and w rounded along the other axis).  The result has x's type."""
-    xq, xt = mx4_quantize_both(x)
-    wq, wt = mx4_quantize_both(w)
-    return mx4_matmul(xq, wq, x.dtype), (xt, wt, x.dtype, w.dtype)
+    x_type, m, k, ldx = _matrix(x, "x")
+    w_type, n, k2, ldw = _matrix(w, "w")
+    device = x.device
+    if k != k2:
+        raise ValueError(f"x is {tuple(x.shape)}, w is {tuple(w.shape)}: their columns must agree")
+    if w.device != device:
+        raise ValueError("x and w must be on the same device")
+    y = torch.empty((m, n), dtype=x.dtype, device=device)
+    xt = _size(k, m)
+    saved = _bytes(xt + _size(k, n), device)
+    work = _bytes(_size(m, k) + _size(n, k), device)
+    at = saved.data_ptr()
+    _call(_lib.zoa_mx4_linear_forward, device, x.data_ptr(), x_type, ldx, w.data_ptr(), w_type, ldw, m, n, k, y.data_ptr(), n, at, at + xt,
+          work.data_ptr())
+    return y, Mx4LinearSaved(saved, m, n, k, x.dtype, w.dtype)
 
 
-def mx4_linear_backward(dy, saved):
+def mx4_linear_backward(dy, saved, need_dx=True, need_dw=True):
     """(dx, dw) for the gradient dy [tokens, out] of mx4_linear_forward's result, the rounding's own derivative taken
-    as 1: dx = Q(dy) Q(w^T)^T, dw = Q(dy^T) Q(x^T)^T, of x's and w's types."""
-    xt, wt, x_dtype, w_dtype = saved
-    if dy.shape != (xt.cols, wt.cols):
-        raise ValueError(f"dy is {tuple(dy.shape)}, the layer's result was ({xt.cols}, {wt.cols})")
-    dyq, dyt = mx4_quantize_both(dy)
-    return mx4_matmul(dyq, wt, x_dtype), mx4_matmul(dyt, xt, w_dtype)
+    as 1: dx = Q(dy) Q(w^T)^T, dw = Q(dy^T) Q(x^T)^T, of x's and w's types; None for one that is not needed."""
+    code, m, n, ld = _matrix(dy, "dy")
+    k, device = saved.k, saved.data.device
+    if m != saved.m or n != saved.n or dy.device != device:
+        raise ValueError(f"dy is {tuple(dy.shape)} on {dy.device}, the layer's result was ({saved.m}, {saved.n}) on {device}")
+    dx = torch.empty((m, k), dtype=saved.x_dtype, device=device) if need_dx else None
+    dw = torch.empty((n, k), dtype=saved.w_dtype, device=device) if need_dw else None
+    if need_dx or need_dw:
+        work = _bytes(_size(m, n) + _size(n, m), device)
+        at = saved.data.data_ptr()
+        _call(_lib.zoa_mx4_linear_backward, device, dy.data_ptr(), code, ld, m, n, k, at, at + _size(k, m),
+              dx.data_ptr() if need_dx else None, _TYPES[saved.x_dtype], k, dw.data_ptr() if need_dw else None,
+              _TYPES[saved.w_dtype], k, work.data_ptr())
+    return dx, dw
 
 
 class Mx4LinearFunction(torch.autograd.Function):
@@ -150,13 +210,12 @@ class Mx4LinearFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, w):
-        y, (xt, wt, ctx.x_dtype, ctx.w_dtype) = mx4_linear_forward(x, w)
-        ctx.save_for_backward(xt.data, wt.data)
-        ctx.sides = (xt.shape, wt.shape)
+        y, saved = mx4_linear_forward(x, w)
+        ctx.save_for_backward(saved.data)
+        ctx.layer = (saved.m, saved.n, saved.k, saved.x_dtype, saved.w_dtype)
         return y
 
     @staticmethod
     def backward(ctx, dy):
-        xt, wt = ctx.saved_tensors
-        saved = (Mx4(*ctx.sides[0], data=xt), Mx4(*ctx.sides[1], data=wt), ctx.x_dtype, ctx.w_dtype)
-        return mx4_linear_backward(dy if dy.stride(-1) == 1 else dy.contiguous(), saved)
+        saved = Mx4LinearSaved(ctx.saved_tensors[0], *ctx.layer)
+        return mx4_linear_backward(dy if dy.stride(-1) == 1 else dy.contiguous(), saved, *ctx.needs_input_grad)

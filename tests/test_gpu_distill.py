@@ -189,14 +189,13 @@ def test_offsets_past_32_bits():
     rows, vocab = 45000, 50257
     p = problem(8, vocab, 8, torch.bfloat16, 7, tail=True, labels=True)
     p["row_weight"] = torch.ones(8, device="cuda")
-    want_loss, want = distill_topk_grad(**p)
     z = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
     z[-8:] = p["logits"]
     fill = lambda t: torch.cat([torch.zeros((rows - 8,) + t.shape[1:], dtype=t.dtype, device="cuda"), t])  # noqa: E731
     big = dict(p, logits=z, index=fill(p["index"]), teacher=fill(p["teacher"]), row_weight=fill(p["row_weight"]),
                labels=fill(p["labels"]), teacher_lse=fill(p["teacher_lse"]))
     loss, grad = distill_topk_grad(**big, out=z)
-    assert torch.equal(loss[-8:], want_loss) and torch.equal(grad[-8:], want)
+    check(p, loss[-8:], grad[-8:])
     assert not loss[:-8].any() and not grad[:16].any() and not grad[-2000:-8].any()
 
 
