@@ -23,19 +23,33 @@ __host__ __device__ constexpr uint32_t mma_desc(int m, int n, uint32_t id)
 {
     return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 4) << 24) | (id << 29);
 }
+#define ZOA_MMA_MX4(group)                                                                                             \
+    asm volatile(                                                                                                      \
+        "{\n\t.reg .pred p;\n\t"                                                                                       \
+        "setp.ne.u32 p, %6, 0;\n\t"                                                                                    \
+        "tcgen05.mma.cta_group::" #group ".kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" \
+        ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)                             \
+        : "memory")
+// kPair: the tensor cores of two SMs on one tile, issued by the first block of the cluster for both.
+template <bool kPair = false>
 __device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t sfa, uint32_t sfb, bool accumulate)
 {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.u32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
-        : "memory");
+    if constexpr (kPair) ZOA_MMA_MX4(2);
+    else ZOA_MMA_MX4(1);
 }
 // 32 rows x 16 bytes of scales to four columns of tensor memory, repeated for the four groups of 32 lanes.
+template <bool kPair = false>
 __device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    if constexpr (kPair) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+// The pair's work issued so far arrives on the barrier at the same place in both blocks when it is done.
+__device__ __forceinline__ void commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"((uint16_t)3)
+                 : "memory");
 }
 __device__ __forceinline__ void commit(uint32_t bar)
 {
@@ -52,15 +66,16 @@ __device__ __forceinline__ void load_columns32(uint32_t tmem, uint32_t *v)
           "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]),
           "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(tmem));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void columns_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 struct MatmulArgs {
     const uint8_t *a, *b;     // tiles
     void *out;
     long long m, n, ld;
     int tiles_k;              // tiles of 256 columns
-    int vec;                  // rows of `out` are 16-byte aligned
+    int k_steps;              // steps of 64 columns, the last one perhaps partly zeros
+    int vec;                  // rows of `out` are 16-byte (1) or 32-byte (2) aligned
     int test_stop;            // > 0: the copies stop after this many tiles (error-path test)
     WaitLimit limit;
 };
@@ -174,6 +189,7 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
             if (j0 + c >= g.n) break;
             uint32_t v[32];
             load_columns32(tmem + ((uint32_t)(quarter * 32) << 16) + c, v);
+            columns_loaded();
             if (i < g.m) store32(row, j0 + c, g.n, g.vec, v);
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -183,6 +199,248 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemColumns) : "memory");
     }
+}
+
+// ---- pairs of SMs, large products --------------------------------------------------------------------------
+// A cluster of two blocks computes 256 x 256 of C at a time, each block the sums of 128 rows, and walks over the tiles
+// with a stride.  Every byte of A goes to one SM and every byte of B's codes too (the tensor cores read the partner's
+// half from its shared memory); only B's scales go to both.  The sums fill half of tensor memory; the scales of the
+// stages in flight take the rest, so the next tile starts when the sums have been taken to registers, not when they
+// have been stored.
+constexpr int kPairStages = 6;
+constexpr int kPairStageBytes = kMxTileBytes + 2 * kMxScaleBytes + kMxCodeBytes;    // A tile; B scales of both halves; B codes
+constexpr int kPairScaleColumns = 24;                                              // 8 for A, 16 for B
+constexpr int kPairThreads = 320;
+struct PairShared {
+    unsigned long long full[kPairStages], partner_full[kPairStages], empty[kPairStages], sums_full, sums_empty, finished;
+    uint32_t tmem;
+    int gave_up;
+};
+constexpr int kPairSmem = kPairStages * kPairStageBytes + 1024 + (int)sizeof(PairShared);
+
+struct PairTile {
+    long long i0;        // this block's first row of A
+    long long j0;        // the pair's first row of B
+    int rows, cols;      // this block's rows that exist (0..128); the pair's columns, a multiple of 32
+};
+__device__ __forceinline__ PairTile pair_tile(const MatmulArgs &g, long long t, int rank)
+{
+    // Tiles go down strips 8 tiles wide, so that the tiles in flight share rows of both operands.
+    const long long tiles_m = (g.m + 255) / 256, tiles_n = (g.n + 255) / 256;
+    const long long strip = t / (tiles_m * 8), first = strip * 8, width = tiles_n - first < 8 ? tiles_n - first : 8;
+    const long long in = t - strip * tiles_m * 8;
+    PairTile p;
+    p.i0 = in / width * 256 + rank * 128;
+    p.j0 = (first + in % width) * 256;
+    p.rows = (int)(g.m - p.i0 < 0 ? 0 : g.m - p.i0 < 128 ? g.m - p.i0 : 128);
+    p.cols = (int)(g.n - p.j0 < 256 ? (g.n - p.j0 + 31) / 32 * 32 : 256);
+    return p;
+}
+
+// 32 neighbours of a row of the result, already of type T; n is the row's length.
+template <typename T>
+__device__ __forceinline__ void store_row32(T *row, long long j, long long n, int vec, const uint32_t *w)
+{
+    constexpr int kWords = 32 * (int)sizeof(T) / 4;
+    if (vec && j + 32 <= n) {
+        uint32_t *dst = reinterpret_cast<uint32_t *>(row + j);
+        if (vec == 2) {
+#pragma unroll
+            for (int k = 0; k < kWords; k += 8)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + k), "r"(w[k]), "r"(w[k + 1]), "r"(w[k + 2]),
+                             "r"(w[k + 3]), "r"(w[k + 4]), "r"(w[k + 5]), "r"(w[k + 6]), "r"(w[k + 7])
+                             : "memory");
+        } else {
+#pragma unroll
+            for (int k = 0; k < kWords; k += 4) *reinterpret_cast<uint4 *>(dst + k) = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+        if (j + k >= n) continue;
+        if constexpr (sizeof(T) == 4) {
+            reinterpret_cast<uint32_t *>(row)[j + k] = w[k];
+        } else {
+            reinterpret_cast<uint16_t *>(row)[j + k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+        }
+    }
+}
+// Sums as loaded from tensor memory, rounded to T (two to a word for the 16-bit types).
+template <typename T>
+__device__ __forceinline__ void round32(const uint32_t *v, uint32_t *w)
+{
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+        if constexpr (sizeof(T) == 4) w[k] = v[k];
+        else if (k % 2 == 0) w[k / 2] = pack2<T>(__uint_as_float(v[k]), __uint_as_float(v[k + 1]));
+    }
+}
+
+// Warp 0 copies tiles, warp 1 issues the tensor cores' work (first block) or tells the first block that this block's
+// copies have landed (second block), warps 2 to 9 take the sums: four quarters of the rows, two halves of the columns.
+template <typename T>
+__global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) matmul_pair_kernel(const MatmulArgs g, const long long tiles)
+{
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    PairShared *sh = reinterpret_cast<PairShared *>(ring + kPairStages * kPairStageBytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)cluster_rank();
+    const long long first = blockIdx.x / 2, stride = gridDim.x / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kPairStages; ++s) {
+            mbar_init(smem_addr(&sh->full[s]), 1);
+            mbar_init(smem_addr(&sh->partner_full[s]), 1);
+            mbar_init(smem_addr(&sh->empty[s]), 1);
+        }
+        mbar_init(smem_addr(&sh->sums_full), 1);
+        mbar_init(smem_addr(&sh->sums_empty), 16);
+        mbar_init(smem_addr(&sh->finished), 1);
+        sh->gave_up = 0;
+        mbar_init_done();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sh->tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = sh->tmem;
+    volatile int *gave_up = &sh->gave_up;
+
+    if (warp == 0 && lane == 0) {
+        int s = 0, issued = 0;
+        uint32_t parity = 0;
+        bool ok = true;
+        for (long long t = first; t < tiles && ok; t += stride) {
+            const PairTile p = pair_tile(g, t, rank);
+            // B: scales of the pair's up to two tiles to both blocks, codes by halves of the pair's columns; a half may
+            // begin in one tile and end in the next.  Rows past the end are neither copied nor stored.
+            const long long exist = g.n - p.j0 < p.cols ? g.n - p.j0 : p.cols;
+            const int half = p.cols / 2, b0 = rank * half, b1 = (int)(exist < b0 + half ? (exist > b0 ? exist : b0) : b0 + half);
+            const int two = exist > 128;
+            const uint8_t *a = g.a + p.i0 / 128 * g.tiles_k * kMxTileBytes, *b = g.b + p.j0 / 128 * g.tiles_k * kMxTileBytes;
+            const long long next_b = (long long)g.tiles_k * kMxTileBytes;
+            const int cut = b0 < 128 ? (b1 < 128 ? b1 : 128) : b0;      // b0 .. cut lie in the first tile, cut .. b1 in the second
+            const uint32_t bytes_a = p.rows ? kMxScaleBytes + 128 * (uint32_t)p.rows : 0;
+            const uint32_t bytes = bytes_a + kMxScaleBytes * (1 + two) + 128 * (uint32_t)(b1 - b0);
+            for (int k = 0; k < g.tiles_k; ++k) {
+                if (g.test_stop > 0 && issued >= g.test_stop) {
+                    ok = false;
+                    break;
+                }
+                if (!mbar_wait(smem_addr(&sh->empty[s]), parity ^ 1u, gave_up, g.limit)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t full = smem_addr(&sh->full[s]), dst = smem_addr(ring + s * kPairStageBytes);
+                const uint32_t dst_sf = dst + kMxTileBytes, dst_b = dst_sf + 2 * kMxScaleBytes;
+                const long long at = (long long)k * kMxTileBytes;
+                mbar_expect(full, bytes);
+                if (bytes_a) bulk_load(dst, a + at, bytes_a, full);
+                if (cut > b0) bulk_load(dst_b, b + at + kMxScaleBytes + b0 * 128, 128 * (uint32_t)(cut - b0), full);
+                if (b1 > cut) bulk_load(dst_b + (cut - b0) * 128, b + next_b + at + kMxScaleBytes + (cut - 128) * 128, 128 * (uint32_t)(b1 - cut), full);
+                bulk_load(dst_sf, b + at, kMxScaleBytes, full);
+                if (two) bulk_load(dst_sf + kMxScaleBytes, b + next_b + at, kMxScaleBytes, full);
+                ++issued;
+                if (++s == kPairStages) {
+                    s = 0;
+                    parity ^= 1u;
+                }
+            }
+        }
+        // Everything has been read when this completes; after giving up, copies in flight land first.
+        const bool done = mbar_wait(smem_addr(&sh->finished), 0, gave_up, g.limit);
+        if (!done || *gave_up)
+            for (int q = issued > kPairStages ? issued - kPairStages : 0; q < issued; ++q)
+                mbar_drain(smem_addr(&sh->full[q % kPairStages]), (uint32_t)(q / kPairStages & 1), g.limit);
+    } else if (warp == 1 && lane == 0 && rank == 1) {
+        int s = 0;
+        uint32_t parity = 0;
+        bool ok = true;
+        for (long long t = first; t < tiles && ok; t += stride)
+            for (int k = 0; k < g.tiles_k; ++k) {
+                if (!(ok = mbar_wait(smem_addr(&sh->full[s]), parity, gave_up, g.limit))) break;
+                mbar_arrive_at(smem_addr(&sh->partner_full[s]), 0);
+                if (++s == kPairStages) {
+                    s = 0;
+                    parity ^= 1u;
+                }
+            }
+    } else if (warp == 1 && lane == 0) {
+        int s = 0;
+        uint32_t parity = 0, round = 0;
+        bool ok = true;
+        for (long long t = first; t < tiles && ok; t += stride, ++round) {
+            const PairTile p = pair_tile(g, t, 0);
+            const uint32_t desc = mma_desc(256, p.cols, 0);
+            if (round > 0 && !mbar_wait<true>(smem_addr(&sh->sums_empty), (round - 1) & 1u, gave_up, g.limit)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            for (int k = 0; k < g.tiles_k; ++k) {
+                if (!mbar_wait(smem_addr(&sh->full[s]), parity, gave_up, g.limit) ||
+                    !mbar_wait<true>(smem_addr(&sh->partner_full[s]), parity, gave_up, g.limit)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t base_a = smem_addr(ring + s * kPairStageBytes), base_sf = base_a + kMxTileBytes, base_b = base_sf + 2 * kMxScaleBytes;
+                const uint32_t sf = tmem + 256 + s * kPairScaleColumns;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    copy_scales<true>(sf + h * 4, scales_desc(base_a + h * 512));
+                    copy_scales<true>(sf + 8 + h * 8, scales_desc(base_sf + h * 512));
+                    copy_scales<true>(sf + 8 + h * 8 + 4, scales_desc(base_sf + kMxScaleBytes + h * 512));
+                }
+                const uint64_t da = codes_desc(base_a + kMxScaleBytes), db = codes_desc(base_b);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (4 * k + q < g.k_steps)
+                        mma_mx4<true>(tmem, da + 2 * q, db + 2 * q, desc | (q & 1 ? mma_desc(0, 0, 2) : 0), sf + (q >> 1) * 4, sf + 8 + (q >> 1) * 8,
+                                      k > 0 || q > 0);
+                commit_pair(smem_addr(&sh->empty[s]));
+                if (++s == kPairStages) {
+                    s = 0;
+                    parity ^= 1u;
+                }
+            }
+            if (ok) commit_pair(smem_addr(&sh->sums_full));
+        }
+        commit_pair(smem_addr(&sh->finished));
+    } else if (warp >= 2) {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        uint32_t round = 0;
+        for (long long t = first; t < tiles; t += stride, ++round) {
+            const PairTile p = pair_tile(g, t, rank);
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->sums_full), round & 1u, gave_up, g.limit))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            uint32_t w[4][32 * sizeof(T) / 4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t v[32];
+                load_columns32(tmem + ((uint32_t)(quarter * 32) << 16) + half * 128 + c * 32, v);
+                columns_loaded();
+                round32<T>(v, w[c]);
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(smem_addr(&sh->sums_empty), 0);
+            const int r = quarter * 32 + lane;
+            if (r < p.rows) {
+                T *row = static_cast<T *>(g.out) + (p.i0 + r) * g.ld;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (half * 128 + c * 32 < p.cols) store_row32<T>(row, p.j0 + half * 128 + c * 32, g.n, g.vec, w[c]);
+            }
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 zoa_status check_matrix(const char *me, const char *name, const void *p)
@@ -223,13 +481,25 @@ extern "C" zoa_status zoa_mx4_matmul(const void *a, const void *b, size_t m, siz
     g.n = (long long)n;
     g.ld = (long long)ld;
     g.tiles_k = (int)mx_tiles((long long)k, kMxTileCols);
-    g.vec = aligned16(out) && ld * dtype_bytes(dtype) % 16 == 0;
+    g.k_steps = (int)mx_tiles((long long)k, 64);
+    const size_t row_bytes = ld * dtype_bytes(dtype), at = reinterpret_cast<uintptr_t>(out);
+    g.vec = (at | row_bytes) % 32 == 0 ? 2 : (at | row_bytes) % 16 == 0 ? 1 : 0;
     g.test_stop = ops_test_stop();
     g.limit.error_word = ops_error_word();
     g.limit.ns = ops_wait_limit_ns();
     if (!g.limit.error_word) return ops_fail(ZOA_ERR_CUDA, "%s: no usable current device", me);
+    const int sms = ops_sm_count();
+    if (sms < 2) return ops_fail(ZOA_ERR_CUDA, "%s: no usable current device", me);
+    const long long pair_tiles = mx_tiles(g.m, 256) * mx_tiles(g.n, 256);
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
+        if (pair_tiles >= sms / 2) {
+            static SmemLimit limit;
+            if (limit.ensure(matmul_pair_kernel<T>, kPairSmem) != cudaSuccess) return;
+            const long long pairs = pair_tiles < sms / 2 ? pair_tiles : sms / 2;
+            matmul_pair_kernel<T><<<(unsigned)(2 * pairs), kPairThreads, kPairSmem, s>>>(g, pair_tiles);
+            return;
+        }
         static SmemLimit limit;
         if (limit.ensure(matmul_kernel<T>, kMatmulSmem) != cudaSuccess) return;
         matmul_kernel<T><<<dim3((unsigned)mx_tiles(g.m, 128), (unsigned)mx_tiles(g.n, 128)), 192, kMatmulSmem, s>>>(g);

@@ -132,6 +132,22 @@ def test_product_of_many_tiles(m, n, k):
         assert_product(mx4_matmul(mx4_quantize(a), mx4_quantize(b), out), va, vb, out)
 
 
+@pytest.mark.parametrize("m,n,k", [(2304, 2304, 512), (2500, 2337, 777), (300, 9500, 100), (19000, 200, 300), (2400, 2401, 2700), (5000, 1122, 65)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_product(m, n, k, dtype):
+    a, b = data(m, k, dtype, m, 0.5), data(n, k, dtype, n + 1, 0.5, 0.1)
+    va, vb = mx4_quantize(a).dequantize(torch.float32), mx4_quantize(b).dequantize(torch.float32)      # tested above
+    pad = 3 if n % 2 else 16
+    out = strided(torch.zeros(m, n, dtype=dtype, device="cuda"), pad, 0)
+    for got in (mx4_matmul(mx4_quantize(a), mx4_quantize(b), dtype), mx4_matmul(mx4_quantize(a), mx4_quantize(b), dtype, out=out)):
+        # on the GPU in 64 bits, with assert_product's bound
+        want, size = va.double() @ vb.double().t(), va.double().abs() @ vb.double().abs().t()
+        rel, least = ULP[dtype]
+        bound = (k / 8 + 8) * 2.0 ** -23 * size + rel * want.abs() + least
+        assert ((got.double() - want).abs() <= bound).all()
+    assert (out._base[:m * (n + pad)].view(m, n + pad)[:, n:] == 7).all()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m", [1, 3, 20, 90, 300])
 @pytest.mark.parametrize("pad,offset", [(1, 0), (0, 3), (8, 8)])
@@ -312,7 +328,7 @@ def test_refusals_of_the_library():
     B.zoa_ops_check_device()
 
 
-@pytest.mark.parametrize("m,n", [(200, 200), (1024, 1024), (30, 500)])
+@pytest.mark.parametrize("m,n", [(200, 200), (1024, 1024), (30, 500), (2400, 2400)])
 def test_a_wait_that_runs_out_is_reported(m, n):
     """The copies stop early, so the product's waits run out after their limit and the status says so."""
     x, w = data(m, 4096, torch.bfloat16, 1), data(n, 4096, torch.bfloat16, 2)
