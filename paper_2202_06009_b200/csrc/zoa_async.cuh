@@ -58,15 +58,19 @@ struct WaitLimit {
 template <bool kCluster = false>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, const WaitLimit &limit)
 {
-    if (mbar_try<kCluster>(bar, parity)) return true;
-    const unsigned long long start = timer_ns();
+    // The clock is first read after many tries: a read takes longer than most waits (it cost a product half its speed).
+    unsigned long long start = 0;
     for (unsigned it = 1;; ++it) {
         if (mbar_try<kCluster>(bar, parity)) return true;
-        if (*gave_up) return false;
-        if ((it & 63u) == 0 && timer_ns() - start > limit.ns) {
-            *gave_up = 1;
-            atomicExch(limit.error_word, 1);
-            return false;
+        if ((it & 255u) == 0) {
+            if (*gave_up) return false;
+            const unsigned long long now = timer_ns();
+            if (start == 0) start = now;
+            if (now - start > limit.ns) {
+                *gave_up = 1;
+                atomicExch(limit.error_word, 1);
+                return false;
+            }
         }
     }
 }
@@ -82,6 +86,13 @@ __device__ __forceinline__ void mbar_arrive_at(uint32_t bar, uint32_t rank)
     uint32_t remote;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(bar), "r"(rank));
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
+}
+// The same without ordering this thread's own earlier writes, which a release at cluster scope waits for.
+__device__ __forceinline__ void mbar_tell(uint32_t bar, uint32_t rank)
+{
+    uint32_t remote;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(bar), "r"(rank));
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {

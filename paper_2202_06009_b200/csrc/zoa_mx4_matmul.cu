@@ -23,37 +23,64 @@ __host__ __device__ constexpr uint32_t mma_desc(int m, int n, uint32_t id)
 {
     return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 4) << 24) | (id << 29);
 }
-#define ZOA_MMA_MX4(group)                                                                                             \
-    asm volatile(                                                                                                      \
-        "{\n\t.reg .pred p;\n\t"                                                                                       \
-        "setp.ne.u32 p, %6, 0;\n\t"                                                                                    \
-        "tcgen05.mma.cta_group::" #group ".kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" \
-        ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)                             \
+// These are called by whole warps and issued by the thread whose `one` is set (elect_one): a branch around them would
+// keep the compiler from holding their operands in uniform registers, which cost 60 to 90 cycles an instruction.
+__device__ __forceinline__ uint32_t elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one;
+}
+#define ZOA_MMA_MX4(group)                                                                                                \
+    asm volatile(                                                                                                         \
+        "{\n\t.reg .pred p, q;\n\t"                                                                                       \
+        "setp.ne.u32 p, %6, 0;\n\t"                                                                                       \
+        "setp.ne.u32 q, %7, 0;\n\t"                                                                                       \
+        "@q tcgen05.mma.cta_group::" #group ".kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" \
+        ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate), "r"(one)                      \
         : "memory")
 // kPair: the tensor cores of two SMs on one tile, issued by the first block of the cluster for both.
 template <bool kPair = false>
-__device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t sfa, uint32_t sfb, bool accumulate)
+__device__ __forceinline__ void mma_mx4(uint32_t one, uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t sfa, uint32_t sfb,
+                                        bool accumulate)
 {
     if constexpr (kPair) ZOA_MMA_MX4(2);
     else ZOA_MMA_MX4(1);
 }
 // 32 rows x 16 bytes of scales to four columns of tensor memory, repeated for the four groups of 32 lanes.
+#define ZOA_IF_ONE(instruction) "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %0, 0;\n\t@q " instruction "\n\t}"
 template <bool kPair = false>
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc)
+__device__ __forceinline__ void copy_scales(uint32_t one, uint32_t tmem, uint64_t desc)
 {
-    if constexpr (kPair) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
-    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    if constexpr (kPair) asm volatile(ZOA_IF_ONE("tcgen05.cp.cta_group::2.32x128b.warpx4 [%1], %2;") ::"r"(one), "r"(tmem), "l"(desc) : "memory");
+    else asm volatile(ZOA_IF_ONE("tcgen05.cp.cta_group::1.32x128b.warpx4 [%1], %2;") ::"r"(one), "r"(tmem), "l"(desc) : "memory");
 }
-// The pair's work issued so far arrives on the barrier at the same place in both blocks when it is done.
-__device__ __forceinline__ void commit_pair(uint32_t bar)
+// The work issued so far arrives on the barrier when it is done; of a pair, at the same place in both blocks.
+__device__ __forceinline__ void commit(uint32_t one, uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                 "h"((uint16_t)3)
+    asm volatile(ZOA_IF_ONE("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];") ::"r"(one), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint32_t one, uint32_t bar)
+{
+    asm volatile(ZOA_IF_ONE("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%1], %2;") ::"r"(one),
+                 "r"(bar), "h"((uint16_t)3)
                  : "memory");
 }
-__device__ __forceinline__ void commit(uint32_t bar)
+__device__ __forceinline__ void expect_one(uint32_t one, uint32_t bar, uint32_t bytes)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile(ZOA_IF_ONE("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%1], %2;") ::"r"(one), "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_load_one(uint32_t one, uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile(ZOA_IF_ONE("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%1], [%2], %3, [%4];") ::"r"(one), "r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+// A bounded wait of a whole warp.
+template <bool kCluster = false>
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, const WaitLimit &limit)
+{
+    return __all_sync(0xffffffffu, mbar_wait<kCluster>(bar, parity, gave_up, limit));
 }
 __device__ __forceinline__ void load_columns32(uint32_t tmem, uint32_t *v)
 {
@@ -67,6 +94,13 @@ __device__ __forceinline__ void load_columns32(uint32_t tmem, uint32_t *v)
           "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(tmem));
 }
+__device__ __forceinline__ void store_columns8(uint32_t tmem, const uint32_t *v)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(tmem), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                 "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+__device__ __forceinline__ void columns_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void columns_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 struct MatmulArgs {
@@ -115,8 +149,8 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
     extern __shared__ __align__(16) unsigned char smem_raw[];
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     MatmulShared *sh = reinterpret_cast<MatmulShared *>(ring + kStages * kStageBytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int issued = 0;           // tiles whose copies thread 0 has started
+    const int warp = (int)__reduce_max_sync(0xffffffffu, threadIdx.x >> 5), lane = threadIdx.x & 31;
+    int issued = 0;           // tiles whose copies warp 0 has started
     const long long i0 = (long long)blockIdx.x * 128, j0 = (long long)blockIdx.y * 128;
 
     if (threadIdx.x == 0) {
@@ -136,10 +170,11 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = sh->tmem;
+    const uint32_t tmem = __reduce_or_sync(0xffffffffu, sh->tmem);       // a uniform register
     volatile int *gave_up = &sh->gave_up;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
+        const uint32_t one = elect_one();
         const uint32_t bytes_a = kMxScaleBytes + 128 * (uint32_t)(g.m - i0 < 128 ? g.m - i0 : 128);
         const uint32_t bytes_b = kMxScaleBytes + 128 * (uint32_t)(g.n - j0 < 128 ? g.n - j0 : 128);
         const uint8_t *a = g.a + (long long)blockIdx.x * g.tiles_k * kMxTileBytes;
@@ -147,36 +182,37 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
         for (int k = 0; k < g.tiles_k; ++k) {
             const int s = k % kStages;
             if (g.test_stop > 0 && k >= g.test_stop) break;
-            if (!mbar_wait(smem_addr(&sh->empty[s]), (uint32_t)(k / kStages & 1) ^ 1u, gave_up, g.limit)) break;
+            if (!warp_wait(smem_addr(&sh->empty[s]), (uint32_t)(k / kStages & 1) ^ 1u, gave_up, g.limit)) break;
             const uint32_t full = smem_addr(&sh->full[s]), dst = smem_addr(ring + s * kStageBytes);
-            mbar_expect(full, bytes_a + bytes_b);
-            bulk_load(dst, a + (long long)k * kMxTileBytes, bytes_a, full);
-            bulk_load(dst + kMxTileBytes, b + (long long)k * kMxTileBytes, bytes_b, full);
+            expect_one(one, full, bytes_a + bytes_b);
+            bulk_load_one(one, dst, a + (long long)k * kMxTileBytes, bytes_a, full);
+            bulk_load_one(one, dst + kMxTileBytes, b + (long long)k * kMxTileBytes, bytes_b, full);
             ++issued;
         }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
+        const uint32_t one = elect_one();
         for (int k = 0; k < g.tiles_k; ++k) {
             const int s = k % kStages;
-            if (!mbar_wait(smem_addr(&sh->full[s]), (uint32_t)(k / kStages & 1), gave_up, g.limit)) break;
+            if (!warp_wait(smem_addr(&sh->full[s]), (uint32_t)(k / kStages & 1), gave_up, g.limit)) break;
             const uint32_t base_a = smem_addr(ring + s * kStageBytes), base_b = base_a + kMxTileBytes;
             const uint32_t sf = tmem + 128 + s * kScaleColumns;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                copy_scales(sf + h * 4, scales_desc(base_a + h * 512));
-                copy_scales(sf + 8 + h * 4, scales_desc(base_b + h * 512));
+                copy_scales(one, sf + h * 4, scales_desc(base_a + h * 512));
+                copy_scales(one, sf + 8 + h * 4, scales_desc(base_b + h * 512));
             }
             const uint64_t da = codes_desc(base_a + kMxScaleBytes), db = codes_desc(base_b + kMxScaleBytes);
 #pragma unroll
             for (int q = 0; q < 4; ++q)      // 64 columns a step: 32 bytes of a 128-byte line
-                mma_mx4(tmem, da + 2 * q, db + 2 * q, q & 1 ? mma_desc(128, 128, 2) : mma_desc(128, 128, 0), sf + (q >> 1) * 4,
+                mma_mx4(one, tmem, da + 2 * q, db + 2 * q, q & 1 ? mma_desc(128, 128, 2) : mma_desc(128, 128, 0), sf + (q >> 1) * 4,
                         sf + 8 + (q >> 1) * 4, k > 0 || q > 0);
-            commit(smem_addr(&sh->empty[s]));
+            commit(one, smem_addr(&sh->empty[s]));
         }
-        commit(smem_addr(&sh->done));
+        commit(one, smem_addr(&sh->done));
     }
     __syncwarp();
     const bool finished = mbar_wait(smem_addr(&sh->done), 0, gave_up, g.limit);
-    if (threadIdx.x == 0 && *gave_up) {      // copies in flight land before the block's shared memory is released
+    if (warp == 0 && *gave_up) {      // copies in flight land before the block's shared memory is released
         for (int q = issued > kStages ? issued - kStages : 0; q < issued; ++q)
             mbar_drain(smem_addr(&sh->full[q % kStages]), (uint32_t)(q / kStages & 1), g.limit);
     }
@@ -210,9 +246,9 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
 constexpr int kPairStages = 6;
 constexpr int kPairStageBytes = kMxTileBytes + 2 * kMxScaleBytes + kMxCodeBytes;    // A tile; B scales of both halves; B codes
 constexpr int kPairScaleColumns = 24;                                              // 8 for A, 16 for B
-constexpr int kPairThreads = 320;
+constexpr int kPairThreads = 448;
 struct PairShared {
-    unsigned long long full[kPairStages], partner_full[kPairStages], empty[kPairStages], sums_full, sums_empty, finished;
+    unsigned long long full[kPairStages], scaled[kPairStages], empty[kPairStages], sums_full, sums_empty, finished;
     uint32_t tmem;
     int gave_up;
 };
@@ -277,21 +313,21 @@ __device__ __forceinline__ void round32(const uint32_t *v, uint32_t *w)
     }
 }
 
-// Warp 0 copies tiles, warp 1 issues the tensor cores' work (first block) or tells the first block that this block's
-// copies have landed (second block), warps 2 to 9 take the sums: four quarters of the rows, two halves of the columns.
+// Warp 0 copies tiles, warps 2 to 5 bring their scales to tensor memory, warp 1 of the first block issues the products,
+// warps 6 to 13 take the sums: four quarters of the rows, two halves of the columns.
 template <typename T>
 __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) matmul_pair_kernel(const MatmulArgs g, const long long tiles)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     PairShared *sh = reinterpret_cast<PairShared *>(ring + kPairStages * kPairStageBytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)cluster_rank();
+    const int warp = (int)__reduce_max_sync(0xffffffffu, threadIdx.x >> 5), lane = threadIdx.x & 31, rank = (int)cluster_rank();
     const long long first = blockIdx.x / 2, stride = gridDim.x / 2;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kPairStages; ++s) {
             mbar_init(smem_addr(&sh->full[s]), 1);
-            mbar_init(smem_addr(&sh->partner_full[s]), 1);
+            mbar_init(smem_addr(&sh->scaled[s]), 8);       // four warps of both blocks
             mbar_init(smem_addr(&sh->empty[s]), 1);
         }
         mbar_init(smem_addr(&sh->sums_full), 1);
@@ -308,10 +344,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
     __syncthreads();
     cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = sh->tmem;
+    const uint32_t tmem = __reduce_or_sync(0xffffffffu, sh->tmem);       // a uniform register
     volatile int *gave_up = &sh->gave_up;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
+        const uint32_t one = elect_one();
         int s = 0, issued = 0;
         uint32_t parity = 0;
         bool ok = true;
@@ -322,29 +359,28 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
             const long long exist = g.n - p.j0 < p.cols ? g.n - p.j0 : p.cols;
             const int half = p.cols / 2, b0 = rank * half, b1 = (int)(exist < b0 + half ? (exist > b0 ? exist : b0) : b0 + half);
             const int two = exist > 128;
-            const uint8_t *a = g.a + p.i0 / 128 * g.tiles_k * kMxTileBytes, *b = g.b + p.j0 / 128 * g.tiles_k * kMxTileBytes;
-            const long long next_b = (long long)g.tiles_k * kMxTileBytes;
             const int cut = b0 < 128 ? (b1 < 128 ? b1 : 128) : b0;      // b0 .. cut lie in the first tile, cut .. b1 in the second
+            const long long next_b = (long long)g.tiles_k * kMxTileBytes;
+            const uint8_t *a = g.a + p.i0 / 128 * next_b, *b = g.b + p.j0 / 128 * next_b;
             const uint32_t bytes_a = p.rows ? kMxScaleBytes + 128 * (uint32_t)p.rows : 0;
-            const uint32_t bytes = bytes_a + kMxScaleBytes * (1 + two) + 128 * (uint32_t)(b1 - b0);
+            const uint32_t bytes_1 = 128 * (uint32_t)(cut - b0), bytes_2 = 128 * (uint32_t)(b1 - cut);
+            const uint32_t bytes = bytes_a + kMxScaleBytes * (1 + two) + bytes_1 + bytes_2;
+            const uint8_t *b_1 = b + kMxScaleBytes + b0 * 128, *b_2 = b + next_b + kMxScaleBytes + (cut - 128) * 128;
             for (int k = 0; k < g.tiles_k; ++k) {
-                if (g.test_stop > 0 && issued >= g.test_stop) {
-                    ok = false;
-                    break;
-                }
-                if (!mbar_wait(smem_addr(&sh->empty[s]), parity ^ 1u, gave_up, g.limit)) {
-                    ok = false;
-                    break;
-                }
+                ok = !(g.test_stop > 0 && issued >= g.test_stop) && warp_wait(smem_addr(&sh->empty[s]), parity ^ 1u, gave_up, g.limit);
+                if (!ok) break;
                 const uint32_t full = smem_addr(&sh->full[s]), dst = smem_addr(ring + s * kPairStageBytes);
                 const uint32_t dst_sf = dst + kMxTileBytes, dst_b = dst_sf + 2 * kMxScaleBytes;
-                const long long at = (long long)k * kMxTileBytes;
-                mbar_expect(full, bytes);
-                if (bytes_a) bulk_load(dst, a + at, bytes_a, full);
-                if (cut > b0) bulk_load(dst_b, b + at + kMxScaleBytes + b0 * 128, 128 * (uint32_t)(cut - b0), full);
-                if (b1 > cut) bulk_load(dst_b + (cut - b0) * 128, b + next_b + at + kMxScaleBytes + (cut - 128) * 128, 128 * (uint32_t)(b1 - cut), full);
-                bulk_load(dst_sf, b + at, kMxScaleBytes, full);
-                if (two) bulk_load(dst_sf + kMxScaleBytes, b + next_b + at, kMxScaleBytes, full);
+                expect_one(one, full, bytes);
+                if (bytes_a) bulk_load_one(one, dst, a, bytes_a, full);
+                if (bytes_1) bulk_load_one(one, dst_b, b_1, bytes_1, full);
+                if (bytes_2) bulk_load_one(one, dst_b + bytes_1, b_2, bytes_2, full);
+                bulk_load_one(one, dst_sf, b, kMxScaleBytes, full);
+                if (two) bulk_load_one(one, dst_sf + kMxScaleBytes, b + next_b, kMxScaleBytes, full);
+                a += kMxTileBytes;
+                b += kMxTileBytes;
+                b_1 += kMxTileBytes;
+                b_2 += kMxTileBytes;
                 ++issued;
                 if (++s == kPairStages) {
                     s = 0;
@@ -353,85 +389,108 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
             }
         }
         // Everything has been read when this completes; after giving up, copies in flight land first.
-        const bool done = mbar_wait(smem_addr(&sh->finished), 0, gave_up, g.limit);
+        const bool done = warp_wait(smem_addr(&sh->finished), 0, gave_up, g.limit);
         if (!done || *gave_up)
             for (int q = issued > kPairStages ? issued - kPairStages : 0; q < issued; ++q)
                 mbar_drain(smem_addr(&sh->full[q % kPairStages]), (uint32_t)(q / kPairStages & 1), g.limit);
-    } else if (warp == 1 && lane == 0 && rank == 1) {
-        int s = 0;
-        uint32_t parity = 0;
-        bool ok = true;
-        for (long long t = first; t < tiles && ok; t += stride)
-            for (int k = 0; k < g.tiles_k; ++k) {
-                if (!(ok = mbar_wait(smem_addr(&sh->full[s]), parity, gave_up, g.limit))) break;
-                mbar_arrive_at(smem_addr(&sh->partner_full[s]), 0);
-                if (++s == kPairStages) {
-                    s = 0;
-                    parity ^= 1u;
-                }
-            }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1 && rank == 0) {
+        const uint32_t one = elect_one();
         int s = 0;
         uint32_t parity = 0, round = 0;
         bool ok = true;
         for (long long t = first; t < tiles && ok; t += stride, ++round) {
             const PairTile p = pair_tile(g, t, 0);
             const uint32_t desc = mma_desc(256, p.cols, 0);
-            if (round > 0 && !mbar_wait<true>(smem_addr(&sh->sums_empty), (round - 1) & 1u, gave_up, g.limit)) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (round > 0 && !warp_wait(smem_addr(&sh->sums_empty), (round - 1) & 1u, gave_up, g.limit)) break;
             for (int k = 0; k < g.tiles_k; ++k) {
-                if (!mbar_wait(smem_addr(&sh->full[s]), parity, gave_up, g.limit) ||
-                    !mbar_wait<true>(smem_addr(&sh->partner_full[s]), parity, gave_up, g.limit)) {
-                    ok = false;
-                    break;
-                }
-                const uint32_t base_a = smem_addr(ring + s * kPairStageBytes), base_sf = base_a + kMxTileBytes, base_b = base_sf + 2 * kMxScaleBytes;
+                // both blocks' copies have landed and their scales are in tensor memory
+                if (!(ok = warp_wait(smem_addr(&sh->scaled[s]), parity, gave_up, g.limit))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t base_a = smem_addr(ring + s * kPairStageBytes), base_b = base_a + kMxTileBytes + 2 * kMxScaleBytes;
                 const uint32_t sf = tmem + 256 + s * kPairScaleColumns;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    copy_scales<true>(sf + h * 4, scales_desc(base_a + h * 512));
-                    copy_scales<true>(sf + 8 + h * 8, scales_desc(base_sf + h * 512));
-                    copy_scales<true>(sf + 8 + h * 8 + 4, scales_desc(base_sf + kMxScaleBytes + h * 512));
-                }
                 const uint64_t da = codes_desc(base_a + kMxScaleBytes), db = codes_desc(base_b);
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     if (4 * k + q < g.k_steps)
-                        mma_mx4<true>(tmem, da + 2 * q, db + 2 * q, desc | (q & 1 ? mma_desc(0, 0, 2) : 0), sf + (q >> 1) * 4, sf + 8 + (q >> 1) * 8,
-                                      k > 0 || q > 0);
-                commit_pair(smem_addr(&sh->empty[s]));
+                        mma_mx4<true>(one, tmem, da + 2 * q, db + 2 * q, desc | (q & 1 ? mma_desc(0, 0, 2) : 0), sf + (q >> 1) * 4,
+                                      sf + 8 + (q >> 1) * 8, k > 0 || q > 0);
+                commit_pair(one, smem_addr(&sh->empty[s]));
                 if (++s == kPairStages) {
                     s = 0;
                     parity ^= 1u;
                 }
             }
-            if (ok) commit_pair(smem_addr(&sh->sums_full));
+            if (ok) commit_pair(one, smem_addr(&sh->sums_full));
         }
-        commit_pair(smem_addr(&sh->finished));
-    } else if (warp >= 2) {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        commit_pair(one, smem_addr(&sh->finished));
+    } else if (warp >= 2 && warp < 6) {
+        // Scales to tensor memory, a warp for each quarter of its lanes.  (The tensor core can copy them itself, but it
+        // does so in line with its products: six copies a stage took as long as two of its four products.)
+        const int quarter = warp & 3;
+        int s = 0;
+        uint32_t parity = 0;
+        bool ok = true;
+        for (long long t = first; t < tiles && ok; t += stride)
+            for (int k = 0; k < g.tiles_k; ++k) {
+                if (!(ok = warp_wait(smem_addr(&sh->full[s]), parity, gave_up, g.limit))) break;
+                const unsigned char *stage = ring + s * kPairStageBytes;
+                const uint4 *a = reinterpret_cast<const uint4 *>(stage) + lane, *b = reinterpret_cast<const uint4 *>(stage + kMxTileBytes) + lane;
+                uint32_t v[24];
+                // columns: A's two groups of 128, then of B for each group its two halves
+                const uint4 w[6] = {a[0], a[32], b[0], b[64], b[32], b[96]};
+#pragma unroll
+                for (int i = 0; i < 6; ++i) {
+                    v[4 * i] = w[i].x;
+                    v[4 * i + 1] = w[i].y;
+                    v[4 * i + 2] = w[i].z;
+                    v[4 * i + 3] = w[i].w;
+                }
+                const uint32_t sf = tmem + ((uint32_t)(quarter * 32) << 16) + 256 + s * kPairScaleColumns;
+                store_columns8(sf, v);
+                store_columns8(sf + 8, v + 8);
+                store_columns8(sf + 16, v + 16);
+                columns_stored();
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    // The stores have been waited for, so nothing is left for a release at cluster scope to order.
+                    if (rank == 0) mbar_arrive(smem_addr(&sh->scaled[s]));
+                    else mbar_tell(smem_addr(&sh->scaled[s]), 0);
+                }
+                if (++s == kPairStages) {
+                    s = 0;
+                    parity ^= 1u;
+                }
+            }
+    } else if (warp >= 6) {
+        const int quarter = warp & 3, half = (warp - 6) >> 2;
         uint32_t round = 0;
         for (long long t = first; t < tiles; t += stride, ++round) {
             const PairTile p = pair_tile(g, t, rank);
             if (!__all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->sums_full), round & 1u, gave_up, g.limit))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            uint32_t w[4][32 * sizeof(T) / 4];
+            // Batches of columns kept for after the release, as many as the registers hold; the others are stored at once.
+            constexpr int kKept = sizeof(T) == 4 ? 2 : 3;
+            const int r = quarter * 32 + lane;
+            T *row = static_cast<T *>(g.out) + (p.i0 + r) * g.ld;
+            uint32_t w[kKept][32 * sizeof(T) / 4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t v[32];
                 load_columns32(tmem + ((uint32_t)(quarter * 32) << 16) + half * 128 + c * 32, v);
                 columns_loaded();
-                round32<T>(v, w[c]);
+                const int at = c < 4 - kKept ? 0 : c - (4 - kKept);
+                round32<T>(v, w[at]);
+                if (c < 4 - kKept && r < p.rows && half * 128 + c * 32 < p.cols) store_row32<T>(row, p.j0 + half * 128 + c * 32, g.n, g.vec, w[at]);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive_at(smem_addr(&sh->sums_empty), 0);
-            const int r = quarter * 32 + lane;
+            // Nothing written here is for the partner: a release would wait for the last tile's stores.
+            if (lane == 0) mbar_tell(smem_addr(&sh->sums_empty), 0);
             if (r < p.rows) {
-                T *row = static_cast<T *>(g.out) + (p.i0 + r) * g.ld;
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (half * 128 + c * 32 < p.cols) store_row32<T>(row, p.j0 + half * 128 + c * 32, g.n, g.vec, w[c]);
+                for (int c = 4 - kKept; c < 4; ++c)
+                    if (half * 128 + c * 32 < p.cols) store_row32<T>(row, p.j0 + half * 128 + c * 32, g.n, g.vec, w[c - (4 - kKept)]);
             }
         }
     }
