@@ -45,22 +45,19 @@ __device__ __forceinline__ float mx_scale(uint32_t byte)
     return byte == 255u ? __uint_as_float(0x7FC00000u) : byte ? __uint_as_float(byte << 23) : __uint_as_float(0x00400000u);
 }
 
-// max that keeps a NaN: |a| as unsigned bits orders finite < inf < NaN.
-__device__ __forceinline__ uint32_t mx_abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-
-// Eight values times `inv` to eight codes, round to nearest even, 6 at most; v[0] in the lowest nibble.
-__device__ __forceinline__ uint32_t mx_codes8(const float *v, float inv)
+// Eight values, already divided by their scale, in four pairs of binary32 (the first in the low half) to eight codes,
+// round to nearest even, 6 at most; the first in the lowest nibble.
+__device__ __forceinline__ uint32_t mx_codes8(const uint64_t *p)
 {
     uint32_t out;
-    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t.reg .f32 x, y;\n\t"
+        "mov.b64 {x, y}, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 a, y, x;\n\t"
+        "mov.b64 {x, y}, %2;\n\tcvt.rn.satfinite.e2m1x2.f32 b, y, x;\n\t"
+        "mov.b64 {x, y}, %3;\n\tcvt.rn.satfinite.e2m1x2.f32 c, y, x;\n\t"
+        "mov.b64 {x, y}, %4;\n\tcvt.rn.satfinite.e2m1x2.f32 d, y, x;\n\t"
         "mov.b32 %0, {a, b, c, d};\n\t}"
         : "=r"(out)
-        : "f"(v[0] * inv), "f"(v[1] * inv), "f"(v[2] * inv), "f"(v[3] * inv), "f"(v[4] * inv), "f"(v[5] * inv), "f"(v[6] * inv),
-          "f"(v[7] * inv));
+        : "l"(p[0]), "l"(p[1]), "l"(p[2]), "l"(p[3]));
     return out;
 }
 

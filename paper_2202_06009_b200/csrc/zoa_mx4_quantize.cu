@@ -7,21 +7,84 @@ namespace {
 constexpr int kRowWarps = 8;      // warps of a block of quantize_rows_kernel
 constexpr int kRowsPerWarp = 4;   // rows whose loads a warp has in flight at once
 
-// Eight neighbours of a row as binary32; columns past `cols` are 0.
+// Eight neighbours of a row as they lie in memory.
 template <typename T>
-__device__ __forceinline__ void load8(const T *row, long long c, long long cols, bool vec, float *v)
+struct Raw8 {
+    static constexpr int kWords = 2 * (int)sizeof(T);
+    uint32_t w[kWords];
+};
+
+// Columns past `cols` are 0.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T *row, long long c, long long cols, bool vec)
 {
+    Raw8<T> r;
     if (vec && c + 8 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-            Vec<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(row + c)), v);
-            Vec<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(row + c + 4)), v + 4);
-        } else {
-            Vec<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(row + c)), v);
+#pragma unroll
+        for (int k = 0; k < Raw8<T>::kWords; k += 4) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(row + c) + k / 4);
+            r.w[k] = v.x;
+            r.w[k + 1] = v.y;
+            r.w[k + 2] = v.z;
+            r.w[k + 3] = v.w;
         }
-        return;
+        return r;
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = c + k < cols ? to_f32(row[c + k]) : 0.0f;
+    for (int k = 0; k < Raw8<T>::kWords; ++k) {
+        if constexpr (sizeof(T) == 4) {
+            r.w[k] = c + k < cols ? reinterpret_cast<const uint32_t *>(row)[c + k] : 0u;
+        } else {
+            const uint16_t *p = reinterpret_cast<const uint16_t *>(row) + c + 2 * k;
+            r.w[k] = (c + 2 * k < cols ? p[0] : 0u) | (c + 2 * k + 1 < cols ? (uint32_t)p[1] << 16 : 0u);
+        }
+    }
+    return r;
+}
+
+// Largest magnitudes as bits, a word for binary32, a half word each for the 16-bit types: magnitudes order as
+// unsigned numbers, finite < inf < NaN, so that a NaN or an infinity wins.
+template <typename T>
+__device__ __forceinline__ uint32_t magnitude(uint32_t w) { return sizeof(T) == 4 ? w & 0x7FFFFFFFu : w & 0x7FFF7FFFu; }
+template <typename T>
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return sizeof(T) == 4 ? max(a, b) : __vmaxu2(a, b); }
+// The magnitude of one element (the low half word of the 16-bit types) as binary32.
+template <typename T>
+__device__ __forceinline__ float magnitude_f32(uint32_t m)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(m);
+    else {
+        float lo, hi;
+        unpack2<T>(m, lo, hi);
+        return lo;
+    }
+}
+
+__device__ __forceinline__ uint64_t times2(uint32_t lo, uint32_t hi, uint64_t by)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"((uint64_t)hi << 32 | lo), "l"(by));
+    return r;
+}
+// A word of two neighbours, or of two rows, times `by`.
+template <typename T>
+__device__ __forceinline__ uint64_t scaled_pair(uint32_t w, uint64_t by)
+{
+    float lo, hi;
+    unpack2<T>(w, lo, hi);
+    return times2(__float_as_uint(lo), __float_as_uint(hi), by);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t codes8(const Raw8<T> &r, float inv)
+{
+    const uint64_t by = (uint64_t)__float_as_uint(inv) << 32 | __float_as_uint(inv);
+    uint64_t p[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (sizeof(T) == 4) p[k] = times2(r.w[2 * k], r.w[2 * k + 1], by);
+        else p[k] = scaled_pair<T>(r.w[k], by);
+    }
+    return mx_codes8(p);
 }
 
 // The 4-byte scale words of a row's two groups of 128 columns, from the scale byte that every lane of block
@@ -34,40 +97,63 @@ __device__ __forceinline__ uint32_t gather_scales(uint32_t byte, int lane)
     return w;
 }
 
-// One warp takes 256 columns (a line of a tile) of kRowsPerWarp rows, a lane 8 neighbours: a block is four lanes.
+// Scale byte of the block that this lane shares with its three neighbours.
+template <typename T>
+__device__ __forceinline__ uint32_t block_scale(const Raw8<T> &r)
+{
+    uint32_t m = magnitude<T>(r.w[0]);
+#pragma unroll
+    for (int k = 1; k < Raw8<T>::kWords; ++k) m = larger<T>(m, magnitude<T>(r.w[k]));
+    if (sizeof(T) == 2) m = max(m & 0xFFFFu, m >> 16);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    return mx_scale_byte(magnitude_f32<T>(m));
+}
+
+// One warp takes 256 columns (a line of a tile) of kRowsPerWarp rows at a time, a lane 8 neighbours: a block is four
+// lanes.  Warps walk over the matrix, the next rows' loads in flight beside this one's arithmetic.
 template <typename T>
 __global__ void __launch_bounds__(kRowWarps * 32) quantize_rows_kernel(const T *__restrict__ x, long long rows, long long cols,
                                                                        long long ld, bool vec, uint8_t *__restrict__ out)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long tile_c = blockIdx.x, tiles_c = gridDim.x;
-    const long long c = tile_c * kMxTileCols + lane * 8;
-    const long long r0 = ((long long)blockIdx.y * kRowWarps + warp) * kRowsPerWarp;
-    float v[kRowsPerWarp][8];
+    const int lane = threadIdx.x & 31;
+    const long long tiles_c = mx_tiles(cols, kMxTileCols), items = mx_tiles(rows, kRowsPerWarp) * tiles_c;
+    const long long stride = (long long)gridDim.x * kRowWarps;
+    long long item = (long long)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+    Raw8<T> next[kRowsPerWarp];
+    auto fetch = [&](long long it) {
+        if (it >= items) return;
+        const long long r0 = it / tiles_c * kRowsPerWarp, c = it % tiles_c * kMxTileCols + lane * 8;
 #pragma unroll
-    for (int i = 0; i < kRowsPerWarp; ++i)
-        if (r0 + i < rows) load8(x + (r0 + i) * ld, c, cols, vec, v[i]);
+        for (int i = 0; i < kRowsPerWarp; ++i)
+            if (r0 + i < rows) next[i] = load8(x + (r0 + i) * ld, c, cols, vec);
+    };
+    fetch(item);
+    for (; item < items; item += stride) {
+        Raw8<T> v[kRowsPerWarp];
 #pragma unroll
-    for (int i = 0; i < kRowsPerWarp; ++i) {
-        const long long r = r0 + i;
-        if (r >= rows) return;
-        uint32_t most = 0;
+        for (int i = 0; i < kRowsPerWarp; ++i) v[i] = next[i];
+        fetch(item + stride);
+        const long long r0 = item / tiles_c * kRowsPerWarp, tile_c = item % tiles_c;
+        uint8_t *tile = out + ((r0 / kMxTileRows) * tiles_c + tile_c) * kMxTileBytes;       // kRowsPerWarp divides its rows
 #pragma unroll
-        for (int k = 0; k < 8; ++k) most = max(most, mx_abs_bits(v[i][k]));
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        const uint32_t byte = mx_scale_byte(__uint_as_float(most));
-        const uint32_t codes = byte == 255u ? 0u : mx_codes8(v[i], mx_inverse(byte));
-        const uint32_t scales = gather_scales(byte, lane);
-        uint8_t *tile = out + ((r / kMxTileRows) * tiles_c + tile_c) * kMxTileBytes;
-        const int rr = (int)(r % kMxTileRows);
-        *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr, lane >> 2) + (lane & 3) * 4) = codes;
-        if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, lane >> 2)) = scales;
+        for (int i = 0; i < kRowsPerWarp; ++i) {
+            if (r0 + i >= rows) break;
+            const uint32_t byte = block_scale(v[i]);
+            const uint32_t codes = byte == 255u ? 0u : codes8(v[i], mx_inverse(byte));
+            const uint32_t scales = gather_scales(byte, lane);
+            const int rr = (int)((r0 + i) % kMxTileRows);
+            *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr, lane >> 2) + (lane & 3) * 4) = codes;
+            if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, lane >> 2)) = scales;
+        }
     }
 }
 
-// One block takes 128 x 128 elements: rounds them along the rows as it loads them, keeps them in shared memory
-// and rounds them along the columns (the rows of the transposed matrix) from there.
+// One block takes 128 x 128 elements: rounds them along the rows as it loads them, keeps them in shared memory and
+// rounds them along the columns (the rows of the transposed matrix) from there, a thread 32 rows of one column (of a
+// pair of columns for the 16-bit types).  Four neighbouring lanes take the four blocks of a column, so that they write
+// 64 bytes of a line together; the columns' places in shared memory are shifted by 8 words for each block of rows, so
+// that those lanes read different banks.
 constexpr int kBothThreads = 256;
 constexpr int kBothSide = 128;
 template <typename T>
@@ -75,75 +161,93 @@ __global__ void __launch_bounds__(kBothThreads) quantize_both_kernel(const T *__
                                                                      long long ld, bool vec, uint8_t *__restrict__ out,
                                                                      uint8_t *__restrict__ out_t)
 {
+    constexpr int kRowWords = kBothSide * (int)sizeof(T) / 4, kPasses = kBothSide / 16;
     extern __shared__ __align__(16) unsigned char both_smem[];
-    T *tile_s = reinterpret_cast<T *>(both_smem);   // [128][128]
+    uint32_t *tile_s = reinterpret_cast<uint32_t *>(both_smem);   // [128][kRowWords]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long c0 = (long long)blockIdx.x * kBothSide, r0 = (long long)blockIdx.y * kBothSide;
     const long long tiles_c = mx_tiles(cols, kMxTileCols), tiles_ct = mx_tiles(rows, kMxTileCols);
     const int half = lane >> 4, l16 = lane & 15;
     const int group = (int)((c0 / kBothSide) & 1);                      // which half of a tile's columns
     uint8_t *tile = out ? out + ((r0 / kMxTileRows) * tiles_c + c0 / kMxTileCols) * kMxTileBytes : nullptr;
+    const bool last_half = group == 0 && c0 + kBothSide >= cols;        // the tile's second half has no block of its own
 
-    // A half warp holds 128 columns of a row.
+    // A half warp holds 128 columns of a row; all loads first.
+    Raw8<T> v[kPasses];
 #pragma unroll
-    for (int i = 0; i < kBothSide / 16; ++i) {
-        const int rr = (warp * (kBothSide / 16) + i) * 2 + half;
-        float v[8];
+    for (int i = 0; i < kPasses; ++i) {
+        const int rr = i * 16 + warp * 2 + half;
         if (r0 + rr < rows) {
-            load8(x + (r0 + rr) * ld, c0 + l16 * 8, cols, vec, v);
+            v[i] = load8(x + (r0 + rr) * ld, c0 + l16 * 8, cols, vec);
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+            for (int k = 0; k < Raw8<T>::kWords; ++k) v[i].w[k] = 0u;
         }
-        T *keep = tile_s + rr * kBothSide + l16 * 8;
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<uint4 *>(keep) = Vec<T>::pack(v);
-            *reinterpret_cast<uint4 *>(keep + 4) = Vec<T>::pack(v + 4);
-        } else {
-            *reinterpret_cast<uint4 *>(keep) = Vec<T>::pack(v);
-        }
-        uint32_t most = 0;
+    }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) most = max(most, mx_abs_bits(v[k]));
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        const uint32_t byte = mx_scale_byte(__uint_as_float(most));
-        const uint32_t codes = byte == 255u ? 0u : mx_codes8(v, mx_inverse(byte));
+    for (int i = 0; i < kPasses; ++i) {
+        const int rr = i * 16 + warp * 2 + half;
+#pragma unroll
+        for (int k = 0; k < Raw8<T>::kWords; k += 4)
+            *reinterpret_cast<uint4 *>(tile_s + rr * kRowWords + ((l16 * Raw8<T>::kWords + k) ^ ((rr >> 5) * 8))) =
+                make_uint4(v[i].w[k], v[i].w[k + 1], v[i].w[k + 2], v[i].w[k + 3]);
+        if (!tile) continue;
+        const uint32_t byte = block_scale(v[i]);
+        const uint32_t codes = byte == 255u ? 0u : codes8(v[i], mx_inverse(byte));
         const uint32_t scales = gather_scales(byte, lane);
-        if (tile && r0 + rr < rows) {
-            const int block = group * 4 + (l16 >> 2);
-            *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr, block) + (l16 & 3) * 4) = codes;
-            if (l16 == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, group * 4)) = scales;
-        }
-        // The last group of a row that ends in a tile's first half also clears the second half.
-        if (tile && r0 + rr < rows && group == 0 && c0 + kBothSide >= cols) {
+        if (r0 + rr >= rows) continue;
+        *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr, group * 4 + (l16 >> 2)) + (l16 & 3) * 4) = codes;
+        if (l16 == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, group * 4)) = scales;
+        if (last_half) {
             *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr, 4 + (l16 >> 2)) + (l16 & 3) * 4) = 0u;
             if (l16 == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, 4)) = 0u;
         }
     }
     __syncthreads();
-    // A thread takes the 32 rows of one block of one column.
     const int group_t = (int)((r0 / kBothSide) & 1);
+    const bool last_half_t = group_t == 0 && r0 + kBothSide >= rows;
     uint8_t *tile_t = out_t + ((c0 / kMxTileRows) * tiles_ct + r0 / kMxTileCols) * kMxTileBytes;
-    for (int item = threadIdx.x; item < kBothSide * 4; item += kBothThreads) {
-        const int cc = item & (kBothSide - 1), blk = item / kBothSide;
-        if (c0 + cc >= cols) continue;
-        float v[32];
-        uint32_t most = 0;
+    const int blk = lane & 3;
+    // One column's codes and scale; the four lanes' scale bytes make a word.
+    auto store_column = [&](int cc, uint32_t byte, uint4 codes) {
+        uint32_t word = byte << (8 * blk);
+        word |= __shfl_xor_sync(0xffffffffu, word, 1);
+        word |= __shfl_xor_sync(0xffffffffu, word, 2);
+        if (c0 + cc >= cols) return;
+        if (byte == 255u) codes = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4 *>(tile_t + mx_code_at(cc, group_t * 4 + blk)) = codes;
+        if (blk == 0) *reinterpret_cast<uint32_t *>(tile_t + mx_scale_at(cc, group_t * 4)) = word;
+        if (last_half_t) {
+            *reinterpret_cast<uint4 *>(tile_t + mx_code_at(cc, 4 + blk)) = make_uint4(0, 0, 0, 0);
+            if (blk == 0) *reinterpret_cast<uint32_t *>(tile_t + mx_scale_at(cc, 4)) = 0u;
+        }
+    };
+    for (int col = threadIdx.x >> 2; col < kRowWords; col += kBothThreads / 4) {     // a word: one column, or a pair
+        uint32_t w[32];
+        uint32_t m = 0;
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
-            v[k] = to_f32(tile_s[(blk * 32 + k) * kBothSide + cc]);
-            most = max(most, mx_abs_bits(v[k]));
+            w[k] = tile_s[(blk * 32 + k) * kRowWords + (col ^ (blk * 8))];
+            m = larger<T>(m, magnitude<T>(w[k]));
         }
-        const uint32_t byte = mx_scale_byte(__uint_as_float(most));
-        const float inv = mx_inverse(byte);
-        uint4 codes = make_uint4(0, 0, 0, 0);
-        if (byte != 255u) codes = make_uint4(mx_codes8(v, inv), mx_codes8(v + 8, inv), mx_codes8(v + 16, inv), mx_codes8(v + 24, inv));
-        *reinterpret_cast<uint4 *>(tile_t + mx_code_at(cc, group_t * 4 + blk)) = codes;
-        tile_t[mx_scale_at(cc, group_t * 4 + blk)] = (uint8_t)byte;
-        if (group_t == 0 && r0 + kBothSide >= rows) {
-            *reinterpret_cast<uint4 *>(tile_t + mx_code_at(cc, 4 + blk)) = make_uint4(0, 0, 0, 0);
-            tile_t[mx_scale_at(cc, 4 + blk)] = 0;
+#pragma unroll
+        for (int h = 0; h < 4 / (int)sizeof(T); ++h) {
+            const uint32_t byte = mx_scale_byte(magnitude_f32<T>(sizeof(T) == 4 ? m : h ? m >> 16 : m & 0xFFFFu));
+            const float inv = mx_inverse(byte);
+            const uint64_t by = (uint64_t)__float_as_uint(inv) << 32 | __float_as_uint(inv);
+            uint32_t codes[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint64_t p[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t a = w[8 * q + 2 * k], c = w[8 * q + 2 * k + 1];
+                    if constexpr (sizeof(T) == 4) p[k] = times2(a, c, by);
+                    else p[k] = scaled_pair<T>(__byte_perm(a, c, h ? 0x7632 : 0x5410), by);
+                }
+                codes[q] = mx_codes8(p);
+            }
+            store_column(sizeof(T) == 4 ? col : 2 * col + h, byte, make_uint4(codes[0], codes[1], codes[2], codes[3]));
         }
     }
 }
@@ -225,21 +329,14 @@ extern "C" zoa_status zoa_mx4_quantize(const void *x, int dtype, size_t rows, si
     const bool vec = rows_vectorised(x, dtype, ld);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const long long R = (long long)rows, C = (long long)cols, L = (long long)ld;
-    zoa_status st = ZOA_OK;
     if (!out_t) {
-        const long long per = kRowWarps * kRowsPerWarp, gy = mx_tiles(R, per);
-        // gridDim.y holds 65535 blocks: a larger matrix takes several launches, whole row tiles each.
-        for (long long y = 0; y < gy && st == ZOA_OK; y += 65532) {
-            const long long n = gy - y < 65532 ? gy - y : 65532, r = y * per;
-            with_type(dtype, [&](auto t) {
-                using T = decltype(t);
-                quantize_rows_kernel<T><<<dim3((unsigned)mx_tiles(C, kMxTileCols), (unsigned)n), kRowWarps * 32, 0, s>>>(
-                    static_cast<const T *>(x) + r * L, R - r, C, L, vec,
-                    static_cast<uint8_t *>(out) + r / kMxTileRows * mx_tiles(C, kMxTileCols) * kMxTileBytes);
-            });
-            st = ops_launched(me);
-        }
-        return st;
+        const long long blocks = mx_tiles(mx_tiles(R, kRowsPerWarp) * mx_tiles(C, kMxTileCols), kRowWarps), most = 4ll * ops_sm_count();
+        with_type(dtype, [&](auto t) {
+            using T = decltype(t);
+            quantize_rows_kernel<T><<<(unsigned)(blocks < most ? blocks : most), kRowWarps * 32, 0, s>>>(static_cast<const T *>(x), R, C, L, vec,
+                                                                                                       static_cast<uint8_t *>(out));
+        });
+        return ops_launched(me);
     }
     if (mx_tiles(R, kBothSide) > 65535) return ops_fail(ZOA_ERR_ARG, "%s: at most 8388480 rows when out_t is asked for", me);
     with_type(dtype, [&](auto t) {
