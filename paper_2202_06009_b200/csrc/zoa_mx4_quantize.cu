@@ -1,6 +1,8 @@
 // Rounding to 4-bit microscaled form (along the rows, along the columns, or both from one read) and reading back.
 #include "zoa_mx4.cuh"
 
+#include <type_traits>
+
 namespace zoa {
 namespace {
 
@@ -14,15 +16,15 @@ struct Raw8 {
     uint32_t w[kWords];
 };
 
-// Columns past `cols` are 0.
+// `have` of the eight exist (0 or less: none); the others are 0.
 template <typename T>
-__device__ __forceinline__ Raw8<T> load8(const T *row, long long c, long long cols, bool vec)
+__device__ __forceinline__ Raw8<T> load8(const T *at, long long have, bool vec)
 {
     Raw8<T> r;
-    if (vec && c + 8 <= cols) {
+    if (vec && have >= 8) {
 #pragma unroll
         for (int k = 0; k < Raw8<T>::kWords; k += 4) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(row + c) + k / 4);
+            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(at) + k / 4);
             r.w[k] = v.x;
             r.w[k + 1] = v.y;
             r.w[k + 2] = v.z;
@@ -33,21 +35,30 @@ __device__ __forceinline__ Raw8<T> load8(const T *row, long long c, long long co
 #pragma unroll
     for (int k = 0; k < Raw8<T>::kWords; ++k) {
         if constexpr (sizeof(T) == 4) {
-            r.w[k] = c + k < cols ? reinterpret_cast<const uint32_t *>(row)[c + k] : 0u;
+            r.w[k] = k < have ? reinterpret_cast<const uint32_t *>(at)[k] : 0u;
         } else {
-            const uint16_t *p = reinterpret_cast<const uint16_t *>(row) + c + 2 * k;
-            r.w[k] = (c + 2 * k < cols ? p[0] : 0u) | (c + 2 * k + 1 < cols ? (uint32_t)p[1] << 16 : 0u);
+            const uint16_t *p = reinterpret_cast<const uint16_t *>(at) + 2 * k;
+            r.w[k] = (2 * k < have ? p[0] : 0u) | (2 * k + 1 < have ? (uint32_t)p[1] << 16 : 0u);
         }
     }
     return r;
 }
 
-// Largest magnitudes as bits, a word for binary32, a half word each for the 16-bit types: magnitudes order as
-// unsigned numbers, finite < inf < NaN, so that a NaN or an infinity wins.
+// The larger of two magnitudes (of each half, for the 16-bit types); a NaN wins.  binary32 compares its bits, which
+// order finite < inf < NaN without their sign.
 template <typename T>
-__device__ __forceinline__ uint32_t magnitude(uint32_t w) { return sizeof(T) == 4 ? w & 0x7FFFFFFFu : w & 0x7FFF7FFFu; }
-template <typename T>
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return sizeof(T) == 4 ? max(a, b) : __vmaxu2(a, b); }
+__device__ __forceinline__ uint32_t larger(uint32_t magnitude, uint32_t w)
+{
+    if constexpr (sizeof(T) == 4) {
+        return max(magnitude, w & 0x7FFFFFFFu);
+    } else {
+        using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+        const T2 r = __hmax2_nan(*reinterpret_cast<const T2 *>(&magnitude), __habs2(*reinterpret_cast<const T2 *>(&w)));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    }
+}
+// Of the two halves of a word of a 16-bit type: bits of magnitudes order like the magnitudes.
+__device__ __forceinline__ uint32_t larger_half(uint32_t m) { return max(m & 0xFFFFu, m >> 16); }
 // The magnitude of one element (the low half word of the 16-bit types) as binary32.
 template <typename T>
 __device__ __forceinline__ float magnitude_f32(uint32_t m)
@@ -66,14 +77,6 @@ __device__ __forceinline__ uint64_t times2(uint32_t lo, uint32_t hi, uint64_t by
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"((uint64_t)hi << 32 | lo), "l"(by));
     return r;
 }
-// A word of two neighbours, or of two rows, times `by`.
-template <typename T>
-__device__ __forceinline__ uint64_t scaled_pair(uint32_t w, uint64_t by)
-{
-    float lo, hi;
-    unpack2<T>(w, lo, hi);
-    return times2(__float_as_uint(lo), __float_as_uint(hi), by);
-}
 template <typename T>
 __device__ __forceinline__ uint32_t codes8(const Raw8<T> &r, float inv)
 {
@@ -81,8 +84,13 @@ __device__ __forceinline__ uint32_t codes8(const Raw8<T> &r, float inv)
     uint64_t p[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        if constexpr (sizeof(T) == 4) p[k] = times2(r.w[2 * k], r.w[2 * k + 1], by);
-        else p[k] = scaled_pair<T>(r.w[k], by);
+        if constexpr (sizeof(T) == 4) {
+            p[k] = times2(r.w[2 * k], r.w[2 * k + 1], by);
+        } else {
+            float lo, hi;
+            unpack2<T>(r.w[k], lo, hi);
+            p[k] = times2(__float_as_uint(lo), __float_as_uint(hi), by);
+        }
     }
     return mx_codes8(p);
 }
@@ -101,10 +109,10 @@ __device__ __forceinline__ uint32_t gather_scales(uint32_t byte, int lane)
 template <typename T>
 __device__ __forceinline__ uint32_t block_scale(const Raw8<T> &r)
 {
-    uint32_t m = magnitude<T>(r.w[0]);
+    uint32_t m = 0;
 #pragma unroll
-    for (int k = 1; k < Raw8<T>::kWords; ++k) m = larger<T>(m, magnitude<T>(r.w[k]));
-    if (sizeof(T) == 2) m = max(m & 0xFFFFu, m >> 16);
+    for (int k = 0; k < Raw8<T>::kWords; ++k) m = larger<T>(m, r.w[k]);
+    if (sizeof(T) == 2) m = larger_half(m);
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
     return mx_scale_byte(magnitude_f32<T>(m));
@@ -117,34 +125,47 @@ __global__ void __launch_bounds__(kRowWarps * 32) quantize_rows_kernel(const T *
                                                                        long long ld, bool vec, uint8_t *__restrict__ out)
 {
     const int lane = threadIdx.x & 31;
-    const long long tiles_c = mx_tiles(cols, kMxTileCols), items = mx_tiles(rows, kRowsPerWarp) * tiles_c;
-    const long long stride = (long long)gridDim.x * kRowWarps;
-    long long item = (long long)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+    const int tiles_c = (int)mx_tiles(cols, kMxTileCols);
+    // A warp's place (rows from r0, tile tile_c) moves on by the number of warps, kept as whole rows of tiles and a rest.
+    const unsigned warps = gridDim.x * kRowWarps, me = blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+    const long long step_rows = (long long)(warps / tiles_c) * kRowsPerWarp;
+    const int step_tiles = (int)(warps % tiles_c);
+    long long next_r0 = (long long)(me / tiles_c) * kRowsPerWarp;
+    int next_tile = (int)(me % tiles_c);
     Raw8<T> next[kRowsPerWarp];
-    auto fetch = [&](long long it) {
-        if (it >= items) return;
-        const long long r0 = it / tiles_c * kRowsPerWarp, c = it % tiles_c * kMxTileCols + lane * 8;
+    auto fetch = [&] {
+        const long long c = (long long)next_tile * kMxTileCols + lane * 8;
+        const T *at = x + next_r0 * ld + c;
 #pragma unroll
-        for (int i = 0; i < kRowsPerWarp; ++i)
-            if (r0 + i < rows) next[i] = load8(x + (r0 + i) * ld, c, cols, vec);
+        for (int i = 0; i < kRowsPerWarp; ++i, at += ld)
+            if (next_r0 + i < rows) next[i] = load8(at, cols - c, vec);
     };
-    fetch(item);
-    for (; item < items; item += stride) {
+    fetch();
+    while (next_r0 < rows) {
         Raw8<T> v[kRowsPerWarp];
 #pragma unroll
         for (int i = 0; i < kRowsPerWarp; ++i) v[i] = next[i];
-        fetch(item + stride);
-        const long long r0 = item / tiles_c * kRowsPerWarp, tile_c = item % tiles_c;
+        const long long r0 = next_r0;
+        const int tile_c = next_tile;
+        next_r0 += step_rows;
+        next_tile += step_tiles;
+        if (next_tile >= tiles_c) {
+            next_tile -= tiles_c;
+            next_r0 += kRowsPerWarp;
+        }
+        fetch();
+        const int there = (int)(rows - r0 < kRowsPerWarp ? rows - r0 : kRowsPerWarp), rr = (int)(r0 % kMxTileRows);
         uint8_t *tile = out + ((r0 / kMxTileRows) * tiles_c + tile_c) * kMxTileBytes;       // kRowsPerWarp divides its rows
+        uint8_t *codes_at = tile + kMxScaleBytes + rr * 128 + (lane & 3) * 4, *scales_at = tile + mx_scale_at(rr, lane >> 2);
+        const int line = ((lane >> 2) ^ (rr & 7)) << 4;
 #pragma unroll
         for (int i = 0; i < kRowsPerWarp; ++i) {
-            if (r0 + i >= rows) break;
+            if (i >= there) break;
             const uint32_t byte = block_scale(v[i]);
             const uint32_t codes = byte == 255u ? 0u : codes8(v[i], mx_inverse(byte));
             const uint32_t scales = gather_scales(byte, lane);
-            const int rr = (int)((r0 + i) % kMxTileRows);
-            *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr, lane >> 2) + (lane & 3) * 4) = codes;
-            if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, lane >> 2)) = scales;
+            *reinterpret_cast<uint32_t *>(codes_at + i * 128 + (line ^ (i << 4))) = codes;
+            if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(scales_at + i * 16) = scales;
         }
     }
 }
@@ -178,7 +199,7 @@ __global__ void __launch_bounds__(kBothThreads) quantize_both_kernel(const T *__
     for (int i = 0; i < kPasses; ++i) {
         const int rr = i * 16 + warp * 2 + half;
         if (r0 + rr < rows) {
-            v[i] = load8(x + (r0 + rr) * ld, c0 + l16 * 8, cols, vec);
+            v[i] = load8(x + (r0 + rr) * ld + c0 + l16 * 8, cols - c0 - l16 * 8, vec);
         } else {
 #pragma unroll
             for (int k = 0; k < Raw8<T>::kWords; ++k) v[i].w[k] = 0u;
@@ -228,31 +249,68 @@ __global__ void __launch_bounds__(kBothThreads) quantize_both_kernel(const T *__
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
             w[k] = tile_s[(blk * 32 + k) * kRowWords + (col ^ (blk * 8))];
-            m = larger<T>(m, magnitude<T>(w[k]));
+            m = larger<T>(m, w[k]);
+        }
+        constexpr int kColumns = 4 / (int)sizeof(T);
+        uint32_t byte[kColumns], codes[kColumns][4];
+        uint64_t by[kColumns];
+#pragma unroll
+        for (int h = 0; h < kColumns; ++h) {
+            byte[h] = mx_scale_byte(magnitude_f32<T>(kColumns == 1 ? m : h ? m >> 16 : m & 0xFFFFu));
+            const float inv = mx_inverse(byte[h]);
+            by[h] = (uint64_t)__float_as_uint(inv) << 32 | __float_as_uint(inv);
         }
 #pragma unroll
-        for (int h = 0; h < 4 / (int)sizeof(T); ++h) {
-            const uint32_t byte = mx_scale_byte(magnitude_f32<T>(sizeof(T) == 4 ? m : h ? m >> 16 : m & 0xFFFFu));
-            const float inv = mx_inverse(byte);
-            const uint64_t by = (uint64_t)__float_as_uint(inv) << 32 | __float_as_uint(inv);
-            uint32_t codes[4];
+        for (int q = 0; q < 4; ++q) {
+            uint64_t p[kColumns][4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                uint64_t p[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t a = w[8 * q + 2 * k], c = w[8 * q + 2 * k + 1];
-                    if constexpr (sizeof(T) == 4) p[k] = times2(a, c, by);
-                    else p[k] = scaled_pair<T>(__byte_perm(a, c, h ? 0x7632 : 0x5410), by);
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t a = w[8 * q + 2 * k], b = w[8 * q + 2 * k + 1];
+                if constexpr (kColumns == 1) {
+                    p[0][k] = times2(a, b, by[0]);
+                } else {
+                    float a0, a1, b0, b1;
+                    unpack2<T>(a, a0, a1);
+                    unpack2<T>(b, b0, b1);
+                    p[0][k] = times2(__float_as_uint(a0), __float_as_uint(b0), by[0]);
+                    p[1][k] = times2(__float_as_uint(a1), __float_as_uint(b1), by[1]);
                 }
-                codes[q] = mx_codes8(p);
             }
-            store_column(sizeof(T) == 4 ? col : 2 * col + h, byte, make_uint4(codes[0], codes[1], codes[2], codes[3]));
+#pragma unroll
+            for (int h = 0; h < kColumns; ++h) codes[h][q] = mx_codes8(p[h]);
         }
+#pragma unroll
+        for (int h = 0; h < kColumns; ++h) store_column(kColumns * col + h, byte[h], make_uint4(codes[h][0], codes[h][1], codes[h][2], codes[h][3]));
     }
 }
 
-// A warp reads 256 columns of a row, a lane the 8 values of one 4-byte word.
+// Eight codes and their scale byte as bfloat16: the bytes of the eight magnitudes (0, 0.5, 1, 1.5, 2, 3, 4, 6 are
+// 0000 3F00 3F80 3FC0 4000 4040 4080 40C0) looked up four at a time, the signs put in, and one exact product by the
+// scale, which bfloat16 holds whatever its exponent.
+__device__ __forceinline__ uint4 values8(uint32_t codes, uint32_t byte)
+{
+    const uint32_t sel = codes & 0x77777777u;
+    uint32_t word[4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t low = __byte_perm(0xC0800000u, 0xC0804000u, sel >> (16 * h)), high = __byte_perm(0x3F3F3F00u, 0x40404040u, sel >> (16 * h));
+        word[2 * h] = __byte_perm(low, high, 0x5140);
+        word[2 * h + 1] = __byte_perm(low, high, 0x7362);
+    }
+    const uint32_t scale = byte == 255u ? 0x7FC0u : byte ? byte << 7 : 0x0040u;
+    const uint32_t scale2 = scale << 16 | scale;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t pair = codes >> (8 * k);
+        word[k] |= (pair << 12 & 0x8000u) | (pair << 24 & 0x80000000u);
+        const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&word[k]), *reinterpret_cast<const __nv_bfloat162 *>(&scale2));
+        word[k] = *reinterpret_cast<const uint32_t *>(&v);
+    }
+    return make_uint4(word[0], word[1], word[2], word[3]);
+}
+
+// A warp reads 256 columns of kReadRows rows, a lane the 8 values of one 4-byte word of each.
+constexpr int kReadRows = 8;
 template <typename T>
 __global__ void __launch_bounds__(kRowWarps * 32) dequantize_kernel(const uint8_t *__restrict__ in, long long rows, long long cols,
                                                                     T *__restrict__ out, long long ld, bool vec)
@@ -260,23 +318,29 @@ __global__ void __launch_bounds__(kRowWarps * 32) dequantize_kernel(const uint8_
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long tile_c = blockIdx.x, tiles_c = gridDim.x;
     const long long c = tile_c * kMxTileCols + lane * 8;
-    const long long r0 = ((long long)blockIdx.y * kRowWarps + warp) * kRowsPerWarp;
-    if (c >= cols) return;
-    uint32_t codes[kRowsPerWarp];
-    uint32_t bytes[kRowsPerWarp];
+    const long long r0 = ((long long)blockIdx.y * kRowWarps + warp) * kReadRows;
+    if (c >= cols || r0 >= rows) return;
+    const int there = (int)(rows - r0 < kReadRows ? rows - r0 : kReadRows), rr = (int)(r0 % kMxTileRows);       // kReadRows divides a tile's rows
+    const uint8_t *tile = in + ((r0 / kMxTileRows) * tiles_c + tile_c) * kMxTileBytes;
+    const uint8_t *codes_at = tile + kMxScaleBytes + rr * 128 + (lane & 3) * 4, *scales_at = tile + mx_scale_at(rr, lane >> 2);
+    uint32_t codes[kReadRows], bytes[kReadRows];
 #pragma unroll
-    for (int i = 0; i < kRowsPerWarp; ++i) {
-        const long long r = r0 + i;
-        if (r >= rows) break;
-        const uint8_t *tile = in + ((r / kMxTileRows) * tiles_c + tile_c) * kMxTileBytes;
-        const int rr = (int)(r % kMxTileRows);
-        codes[i] = __ldg(reinterpret_cast<const uint32_t *>(tile + mx_code_at(rr, lane >> 2) + (lane & 3) * 4));
-        bytes[i] = __ldg(tile + mx_scale_at(rr, lane >> 2));
+    for (int i = 0; i < kReadRows; ++i) {
+        if (i >= there) break;
+        codes[i] = __ldg(reinterpret_cast<const uint32_t *>(codes_at + i * 128 + (((lane >> 2) ^ i) << 4)));
+        bytes[i] = __ldg(scales_at + i * 16);
     }
+    const bool whole = vec && c + 8 <= cols;
+    T *dst = out + r0 * ld + c;
 #pragma unroll
-    for (int i = 0; i < kRowsPerWarp; ++i) {
-        const long long r = r0 + i;
-        if (r >= rows) break;
+    for (int i = 0; i < kReadRows; ++i, dst += ld) {
+        if (i >= there) break;
+        if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+            if (whole) {
+                *reinterpret_cast<uint4 *>(dst) = values8(codes[i], bytes[i]);
+                continue;
+            }
+        }
         const float s = mx_scale(bytes[i]);
         float v[8];
 #pragma unroll
@@ -290,8 +354,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) dequantize_kernel(const uint8_
             v[2 * k] = lo * s;
             v[2 * k + 1] = hi * s;
         }
-        T *dst = out + r * ld + c;
-        if (vec && c + 8 <= cols) {
+        if (whole) {
             *reinterpret_cast<uint4 *>(dst) = Vec<T>::pack(v);
             if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4 *>(dst + 4) = Vec<T>::pack(v + 4);
         } else {
@@ -363,8 +426,9 @@ extern "C" zoa_status zoa_mx4_dequantize(const void *q, size_t rows, size_t cols
     if (!aligned16(q)) return ops_fail(ZOA_ERR_ARG, "%s: q must be 16-byte aligned", me);
     if (reinterpret_cast<uintptr_t>(out) % dtype_bytes(dtype)) return ops_fail(ZOA_ERR_ARG, "%s: out is not aligned to its element type", me);
     const bool vec = rows_vectorised(out, dtype, ld);
-    const long long R = (long long)rows, C = (long long)cols, L = (long long)ld, per = kRowWarps * kRowsPerWarp, gy = mx_tiles(R, per);
+    const long long R = (long long)rows, C = (long long)cols, L = (long long)ld, per = kRowWarps * kReadRows, gy = mx_tiles(R, per);
     zoa_status st = ZOA_OK;
+    // gridDim.y holds 65535 blocks: a larger matrix takes several launches, whole row tiles each.
     for (long long y = 0; y < gy && st == ZOA_OK; y += 65532) {
         const long long n = gy - y < 65532 ? gy - y : 65532, r = y * per;
         with_type(dtype, [&](auto t) {
