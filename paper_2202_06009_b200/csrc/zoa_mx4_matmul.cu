@@ -110,60 +110,66 @@ struct MatmulArgs {
     int tiles_k;              // tiles of 256 columns
     int k_steps;              // steps of 64 columns, the last one perhaps partly zeros
     int vec;                  // rows of `out` are 16-byte (1) or 32-byte (2) aligned
-    int test_stop;            // > 0: the copies stop after this many tiles (error-path test)
+    int test_stop;            // > 0: the copies stop at this k tile (error-path test)
     WaitLimit limit;
 };
 
-constexpr int kStages = 6;
-constexpr int kStageBytes = 2 * kMxTileBytes;
-constexpr int kTmemColumns = 256;                    // 128 of sums, then 16 of scales per stage
-constexpr int kScaleColumns = 16;
-struct MatmulShared {
-    unsigned long long full[kStages], empty[kStages], done;
-    uint32_t tmem;
-    int gave_up;
+// ---- one SM a tile, small products --------------------------------------------------------------------------
+// A block computes 128 x kBN of C, or its share of the sum over k: the `splits` blocks of a cluster divide the k tiles
+// and add their sums up through each other's shared memory, in the order of their ranks.  Narrow tiles and splits put a
+// product of few rows on all SMs, where its time is that of reading one operand.
+template <int kBN>
+struct Small {
+    static_assert(kBN == 64 || kBN == 128, "scales begin at even columns");
+    static constexpr int kStages = kBN == 128 ? 3 : 4;
+    static constexpr int kStageBytes = kMxTileBytes + kMxScaleBytes + kBN * 128;       // A tile; B scales; B codes
+    static constexpr int kScaleColumns = 16;                                           // 8 for A, 8 for B
+    static constexpr int kTmemColumns = kBN + 16 * kStages > 256 ? 512 : 256;
+    static constexpr int kPitch = kBN + 4;          // floats; rows 4 banks apart
+    struct Shared {
+        unsigned long long full[kStages], empty[kStages], done;
+        uint32_t tmem;
+        int gave_up;
+    };
+    static constexpr int kSmem = kStages * kStageBytes + 1024 + (int)sizeof(Shared);
 };
-constexpr int kMatmulSmem = kStages * kStageBytes + 1024 + (int)sizeof(MatmulShared);
 
-template <typename T>
-__device__ __forceinline__ void store32(T *row, long long j, long long n, bool vec, const uint32_t *w)
+__device__ __forceinline__ float4 load_from_block(uint32_t addr, uint32_t rank)
 {
-    float v[32];
-#pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(w[k]);
-    if (vec && j + 32 <= n) {
-#pragma unroll
-        for (int k = 0; k < 32; k += Vec<T>::kElems) *reinterpret_cast<uint4 *>(row + j + k) = Vec<T>::pack(v + k);
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 32; ++k)
-        if (j + k < n) row[j + k] = from_f32<T>(v[k]);
+    uint32_t remote;
+    float4 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
+    return v;
 }
 
-// One block computes 128 x 128 of C.  Warp 0 copies tiles into the ring, warp 1 issues the tensor core's work,
-// warps 2 to 5 store the result.
-template <typename T>
-__global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
+// Warp 0 copies tiles into the ring, warp 1 issues the tensor core's work, warps 2 to 5 take the sums; all store.
+template <typename T, int kBN>
+__global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g, const int splits, const int tiles_n)
 {
+    using S = Small<kBN>;
     extern __shared__ __align__(16) unsigned char smem_raw[];
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    MatmulShared *sh = reinterpret_cast<MatmulShared *>(ring + kStages * kStageBytes);
+    typename S::Shared *sh = reinterpret_cast<typename S::Shared *>(ring + S::kStages * S::kStageBytes);
     const int warp = (int)__reduce_max_sync(0xffffffffu, threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int split = splits > 1 ? (int)(blockIdx.x % (unsigned)splits) : 0;
+    const unsigned tile = blockIdx.x / (unsigned)splits;
+    const long long i0 = (long long)(tile / (unsigned)tiles_n) * 128, j0 = (long long)(tile % (unsigned)tiles_n) * kBN;
+    const int k0 = (int)((long long)g.tiles_k * split / splits), k1 = (int)((long long)g.tiles_k * (split + 1) / splits);
+    const int rows = (int)(g.m - i0 < 128 ? g.m - i0 : 128), cols = (int)(g.n - j0 < kBN ? g.n - j0 : kBN);
     int issued = 0;           // tiles whose copies warp 0 has started
-    const long long i0 = (long long)blockIdx.x * 128, j0 = (long long)blockIdx.y * 128;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < S::kStages; ++s) {
             mbar_init(smem_addr(&sh->full[s]), 1);
             mbar_init(smem_addr(&sh->empty[s]), 1);
         }
         mbar_init(smem_addr(&sh->done), 1);
         sh->gave_up = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        mbar_init_done();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh->tmem)), "r"(kTmemColumns)
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh->tmem)), "n"(S::kTmemColumns)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -175,27 +181,39 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
 
     if (warp == 0) {
         const uint32_t one = elect_one();
-        const uint32_t bytes_a = kMxScaleBytes + 128 * (uint32_t)(g.m - i0 < 128 ? g.m - i0 : 128);
-        const uint32_t bytes_b = kMxScaleBytes + 128 * (uint32_t)(g.n - j0 < 128 ? g.n - j0 : 128);
-        const uint8_t *a = g.a + (long long)blockIdx.x * g.tiles_k * kMxTileBytes;
-        const uint8_t *b = g.b + (long long)blockIdx.y * g.tiles_k * kMxTileBytes;
-        for (int k = 0; k < g.tiles_k; ++k) {
-            const int s = k % kStages;
+        const int row_b = (int)(j0 % kMxTileRows);      // this block's first row in its tile of B
+        const uint32_t bytes_a = kMxScaleBytes + 128 * (uint32_t)rows, bytes_b = 128 * (uint32_t)cols;
+        const uint8_t *a = g.a + (i0 / kMxTileRows * g.tiles_k + k0) * kMxTileBytes;
+        const uint8_t *b = g.b + (j0 / kMxTileRows * g.tiles_k + k0) * kMxTileBytes;
+        int s = 0;
+        uint32_t parity = 1;
+        for (int k = k0; k < k1; ++k) {
             if (g.test_stop > 0 && k >= g.test_stop) break;
-            if (!warp_wait(smem_addr(&sh->empty[s]), (uint32_t)(k / kStages & 1) ^ 1u, gave_up, g.limit)) break;
-            const uint32_t full = smem_addr(&sh->full[s]), dst = smem_addr(ring + s * kStageBytes);
-            expect_one(one, full, bytes_a + bytes_b);
-            bulk_load_one(one, dst, a + (long long)k * kMxTileBytes, bytes_a, full);
-            bulk_load_one(one, dst + kMxTileBytes, b + (long long)k * kMxTileBytes, bytes_b, full);
+            if (!warp_wait(smem_addr(&sh->empty[s]), parity, gave_up, g.limit)) break;
+            const uint32_t full = smem_addr(&sh->full[s]), dst = smem_addr(ring + s * S::kStageBytes);
+            expect_one(one, full, bytes_a + kMxScaleBytes + bytes_b);
+            bulk_load_one(one, dst, a, bytes_a, full);
+            bulk_load_one(one, dst + kMxTileBytes, b, kMxScaleBytes, full);
+            bulk_load_one(one, dst + kMxTileBytes + kMxScaleBytes, b + kMxScaleBytes + row_b * 128, bytes_b, full);
+            a += kMxTileBytes;
+            b += kMxTileBytes;
             ++issued;
+            if (++s == S::kStages) {
+                s = 0;
+                parity ^= 1u;
+            }
         }
     } else if (warp == 1) {
         const uint32_t one = elect_one();
-        for (int k = 0; k < g.tiles_k; ++k) {
-            const int s = k % kStages;
-            if (!warp_wait(smem_addr(&sh->full[s]), (uint32_t)(k / kStages & 1), gave_up, g.limit)) break;
-            const uint32_t base_a = smem_addr(ring + s * kStageBytes), base_b = base_a + kMxTileBytes;
-            const uint32_t sf = tmem + 128 + s * kScaleColumns;
+        // The column of the scales of this block's first row: 0 or 2.  (Scales begin at even columns; tiles of 32 columns
+        // would begin at odd ones.)
+        const uint32_t column_b = (uint32_t)(j0 % kMxTileRows) / 32;
+        int s = 0;
+        uint32_t parity = 0;
+        for (int k = k0; k < k1; ++k) {
+            if (!warp_wait(smem_addr(&sh->full[s]), parity, gave_up, g.limit)) break;
+            const uint32_t base_a = smem_addr(ring + s * S::kStageBytes), base_b = base_a + kMxTileBytes;
+            const uint32_t sf = tmem + kBN + s * S::kScaleColumns;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 copy_scales(one, sf + h * 4, scales_desc(base_a + h * 512));
@@ -204,36 +222,76 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
             const uint64_t da = codes_desc(base_a + kMxScaleBytes), db = codes_desc(base_b + kMxScaleBytes);
 #pragma unroll
             for (int q = 0; q < 4; ++q)      // 64 columns a step: 32 bytes of a 128-byte line
-                mma_mx4(one, tmem, da + 2 * q, db + 2 * q, q & 1 ? mma_desc(128, 128, 2) : mma_desc(128, 128, 0), sf + (q >> 1) * 4,
-                        sf + 8 + (q >> 1) * 4, k > 0 || q > 0);
+                if (4 * k + q < g.k_steps)
+                    mma_mx4(one, tmem, da + 2 * q, db + 2 * q, q & 1 ? mma_desc(128, kBN, 2) : mma_desc(128, kBN, 0), sf + (q >> 1) * 4,
+                            sf + 8 + (q >> 1) * 4 + column_b, k > k0 || q > 0);
             commit(one, smem_addr(&sh->empty[s]));
+            if (++s == S::kStages) {
+                s = 0;
+                parity ^= 1u;
+            }
         }
         commit(one, smem_addr(&sh->done));
     }
-    __syncwarp();
-    const bool finished = mbar_wait(smem_addr(&sh->done), 0, gave_up, g.limit);
-    if (warp == 0 && *gave_up) {      // copies in flight land before the block's shared memory is released
-        for (int q = issued > kStages ? issued - kStages : 0; q < issued; ++q)
-            mbar_drain(smem_addr(&sh->full[q % kStages]), (uint32_t)(q / kStages & 1), g.limit);
+    const bool finished = warp_wait(smem_addr(&sh->done), 0, gave_up, g.limit);
+    if (warp == 0 && *gave_up) {      // copies in flight land before the block's shared memory is used otherwise
+        for (int q = issued > S::kStages ? issued - S::kStages : 0; q < issued; ++q)
+            mbar_drain(smem_addr(&sh->full[q % S::kStages]), (uint32_t)(q / S::kStages & 1), g.limit);
     }
-    if (warp >= 2 && finished && !*gave_up) {
+    __syncthreads();
+    // The ring is free: the sums go there, so that rows can be stored by neighbouring threads whatever their alignment.
+    float *sums = reinterpret_cast<float *>(ring);
+    if (warp >= 2 && finished) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const int quarter = warp & 3;
-        const long long i = i0 + quarter * 32 + lane;
-        T *row = static_cast<T *>(g.out) + i * g.ld;
-        for (int c = 0; c < 128; c += 32) {
-            if (j0 + c >= g.n) break;
+        float *mine = sums + (quarter * 32 + lane) * S::kPitch;
+#pragma unroll
+        for (int c = 0; c < kBN; c += 32) {
             uint32_t v[32];
             load_columns32(tmem + ((uint32_t)(quarter * 32) << 16) + c, v);
             columns_loaded();
-            if (i < g.m) store32(row, j0 + c, g.n, g.vec, v);
+#pragma unroll
+            for (int k = 0; k < 32; k += 4) *reinterpret_cast<uint4 *>(mine + c + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
     __syncthreads();
+    if (splits > 1) cluster_sync();
+    // This block's rows of the result: all of them, or its share of the cluster's.
+    const int r0 = rows * split / splits, r1 = rows * (split + 1) / splits;
+    for (int x = threadIdx.x; x < (r1 - r0) * (kBN / 4); x += 192) {
+        const int r = r0 + x / (kBN / 4), c = x % (kBN / 4) * 4;
+        if (c >= cols) continue;
+        float4 v;
+        if (splits == 1) {
+            v = *reinterpret_cast<const float4 *>(sums + r * S::kPitch + c);
+        } else {
+            const uint32_t at = smem_addr(sums + r * S::kPitch + c);
+            v = load_from_block(at, 0);
+            for (int o = 1; o < splits; ++o) {
+                const float4 w = load_from_block(at, (uint32_t)o);
+                v.x += w.x;
+                v.y += w.y;
+                v.z += w.z;
+                v.w += w.w;
+            }
+        }
+        T *dst = static_cast<T *>(g.out) + (i0 + r) * g.ld + j0 + c;
+        if (g.vec && c + 4 <= cols) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst) = v;
+            else *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<T>(v.x, v.y), pack2<T>(v.z, v.w));
+        } else {
+            dst[0] = from_f32<T>(v.x);
+            if (c + 1 < cols) dst[1] = from_f32<T>(v.y);
+            if (c + 2 < cols) dst[2] = from_f32<T>(v.z);
+            if (c + 3 < cols) dst[3] = from_f32<T>(v.w);
+        }
+    }
+    __syncthreads();
+    if (splits > 1) cluster_sync();      // nobody leaves while others read its sums
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemColumns) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kTmemColumns) : "memory");
     }
 }
 
@@ -243,7 +301,7 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g)
 // half from its shared memory); only B's scales go to both.  The sums fill half of tensor memory; the scales of the
 // stages in flight take the rest, so the next tile starts when the sums have been taken to registers, not when they
 // have been stored.
-constexpr int kPairStages = 6;
+constexpr int kPairStages = 5;
 constexpr int kPairStageBytes = kMxTileBytes + 2 * kMxScaleBytes + kMxCodeBytes;    // A tile; B scales of both halves; B codes
 constexpr int kPairScaleColumns = 24;                                              // 8 for A, 16 for B
 constexpr int kPairThreads = 448;
@@ -252,7 +310,8 @@ struct PairShared {
     uint32_t tmem;
     int gave_up;
 };
-constexpr int kPairSmem = kPairStages * kPairStageBytes + 1024 + (int)sizeof(PairShared);
+constexpr int kTurnPitch = 33;                       // floats; a warp's 32 x 32 sums, turned so that lanes hold neighbours
+constexpr int kPairSmem = kPairStages * kPairStageBytes + 1024 + (int)sizeof(PairShared) + 8 * 32 * kTurnPitch * 4;
 
 struct PairTile {
     long long i0;        // this block's first row of A
@@ -273,34 +332,44 @@ __device__ __forceinline__ PairTile pair_tile(const MatmulArgs &g, long long t, 
     return p;
 }
 
-// 32 neighbours of a row of the result, already of type T; n is the row's length.
+// 32 neighbours of a row of the result, already of type T, where rows are aligned and hold all of them.
 template <typename T>
-__device__ __forceinline__ void store_row32(T *row, long long j, long long n, int vec, const uint32_t *w)
+__device__ __forceinline__ void store_row32(T *at, int vec, const uint32_t *w)
 {
     constexpr int kWords = 32 * (int)sizeof(T) / 4;
-    if (vec && j + 32 <= n) {
-        uint32_t *dst = reinterpret_cast<uint32_t *>(row + j);
-        if (vec == 2) {
+    uint32_t *dst = reinterpret_cast<uint32_t *>(at);
+    if (vec == 2) {
 #pragma unroll
-            for (int k = 0; k < kWords; k += 8)
-                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + k), "r"(w[k]), "r"(w[k + 1]), "r"(w[k + 2]),
-                             "r"(w[k + 3]), "r"(w[k + 4]), "r"(w[k + 5]), "r"(w[k + 6]), "r"(w[k + 7])
-                             : "memory");
-        } else {
+        for (int k = 0; k < kWords; k += 8)
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + k), "r"(w[k]), "r"(w[k + 1]), "r"(w[k + 2]),
+                         "r"(w[k + 3]), "r"(w[k + 4]), "r"(w[k + 5]), "r"(w[k + 6]), "r"(w[k + 7])
+                         : "memory");
+    } else {
 #pragma unroll
-            for (int k = 0; k < kWords; k += 4) *reinterpret_cast<uint4 *>(dst + k) = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
-        }
-        return;
+        for (int k = 0; k < kWords; k += 4) *reinterpret_cast<uint4 *>(dst + k) = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
     }
+}
+// Any other 32 columns of a warp's 32 rows (lane = row), turned through shared memory so that a store takes neighbours.
+template <typename T>
+__device__ __forceinline__ void store_turned(T *first, long long ld, int rows, int cols, const uint32_t *w, float *turn)
+{
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
 #pragma unroll
     for (int k = 0; k < 32; ++k) {
-        if (j + k >= n) continue;
+        float v;
         if constexpr (sizeof(T) == 4) {
-            reinterpret_cast<uint32_t *>(row)[j + k] = w[k];
+            v = __uint_as_float(w[k]);
         } else {
-            reinterpret_cast<uint16_t *>(row)[j + k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+            float lo, hi;
+            unpack2<T>(w[k >> 1], lo, hi);
+            v = k & 1 ? hi : lo;
         }
+        turn[lane * kTurnPitch + k] = v;
     }
+    __syncwarp();
+    if (lane < cols)
+        for (int r = 0; r < rows; ++r) first[r * ld + lane] = from_f32<T>(turn[r * kTurnPitch + lane]);
 }
 // Sums as loaded from tensor memory, rounded to T (two to a word for the 16-bit types).
 template <typename T>
@@ -464,6 +533,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
             }
     } else if (warp >= 6) {
         const int quarter = warp & 3, half = (warp - 6) >> 2;
+        float *turn = reinterpret_cast<float *>(sh + 1) + (warp - 6) * 32 * kTurnPitch;
         uint32_t round = 0;
         for (long long t = first; t < tiles; t += stride, ++round) {
             const PairTile p = pair_tile(g, t, rank);
@@ -471,8 +541,17 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             // Batches of columns kept for after the release, as many as the registers hold; the others are stored at once.
             constexpr int kKept = sizeof(T) == 4 ? 2 : 3;
-            const int r = quarter * 32 + lane;
-            T *row = static_cast<T *>(g.out) + (p.i0 + r) * g.ld;
+            const int here = p.rows - quarter * 32 < 32 ? p.rows - quarter * 32 : 32;       // of this warp's rows
+            T *corner = static_cast<T *>(g.out) + (p.i0 + quarter * 32) * g.ld + p.j0;
+            auto store = [&](int c, const uint32_t *w) {
+                const int col = half * 128 + c * 32, have = (int)(g.n - p.j0 - col < 32 ? g.n - p.j0 - col : 32);
+                if (have <= 0 || here <= 0) return;
+                if (g.vec && have == 32) {
+                    if (lane < here) store_row32<T>(corner + lane * g.ld + col, g.vec, w);
+                } else {
+                    store_turned<T>(corner + col, g.ld, here, have, w, turn);
+                }
+            };
             uint32_t w[kKept][32 * sizeof(T) / 4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -481,17 +560,14 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
                 columns_loaded();
                 const int at = c < 4 - kKept ? 0 : c - (4 - kKept);
                 round32<T>(v, w[at]);
-                if (c < 4 - kKept && r < p.rows && half * 128 + c * 32 < p.cols) store_row32<T>(row, p.j0 + half * 128 + c * 32, g.n, g.vec, w[at]);
+                if (c < 4 - kKept) store(c, w[at]);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             // Nothing written here is for the partner: a release would wait for the last tile's stores.
             if (lane == 0) mbar_tell(smem_addr(&sh->sums_empty), 0);
-            if (r < p.rows) {
 #pragma unroll
-                for (int c = 4 - kKept; c < 4; ++c)
-                    if (half * 128 + c * 32 < p.cols) store_row32<T>(row, p.j0 + half * 128 + c * 32, g.n, g.vec, w[c - (4 - kKept)]);
-            }
+            for (int c = 4 - kKept; c < 4; ++c) store(c, w[c - (4 - kKept)]);
         }
     }
     __syncwarp();
@@ -500,6 +576,64 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
     cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// Which kernel, how wide a tile, how many splits: the least time by what the kernels measured on one B200 (launches
+// back to back, in tenths of a microsecond): a pair tile 4.3 per k tile + 15, and 45 once; a tile of 128 (64) columns 4
+// (3.2) per k tile + 45 (35), and 10 once; two blocks to an SM 1.4 times as long per k tile and 10 more; splits 18.
+// E.g. 1024 x 4096 x 1024 by pairs 7.7 us, 128 columns 9.0, 64 columns 12.2; 77 x 1600 x 6400 by 64 columns and 4 splits
+// 7.6, 1 split 11.9, 128 columns and 8 splits 8.2, 1 split 12.9.
+struct ProductPlan {
+    int columns, splits;       // columns 256: pairs of SMs
+};
+ProductPlan product_plan(const MatmulArgs &g, int sms)
+{
+    const double pair_tiles = (double)mx_tiles(g.m, 256) * (double)mx_tiles(g.n, 256);
+    ProductPlan best{256, 1};
+    double least = (double)(long long)((pair_tiles + sms / 2 - 1) / (sms / 2)) * (4.3 * g.tiles_k + 15.0) + 45.0;
+    for (int columns = 128; columns >= 64; columns /= 2)
+        for (int splits = 1; splits <= 8 && splits <= g.tiles_k; splits *= 2) {
+            const double blocks = (double)mx_tiles(g.m, 128) * (double)mx_tiles(g.n, columns) * splits;
+            if (blocks > 1e6) continue;
+            const double rounds = (double)(long long)((blocks + 2 * sms - 1) / (2 * sms)), tiles = (double)((g.tiles_k + splits - 1) / splits);
+            const bool shared = blocks > sms;
+            const double time = rounds * (tiles * (columns == 128 ? 4.0 : 3.2) * (shared ? 1.4 : 1.0) + (columns == 128 ? 45.0 : 35.0)) + 10.0 +
+                                (shared ? 10.0 : 0.0) + (splits > 1 ? 18.0 : 0.0);
+            if (time < least) {
+                least = time;
+                best = ProductPlan{columns, splits};
+            }
+        }
+    return best;
+}
+
+template <typename T, int kBN>
+void launch_small(const MatmulArgs &g, int splits, cudaStream_t s)
+{
+    static SmemLimit limit;
+    auto kernel = matmul_kernel<T, kBN>;
+    if (limit.ensure(kernel, Small<kBN>::kSmem) != cudaSuccess) return;       // the caller reports it
+    const int tiles_n = (int)mx_tiles(g.n, kBN);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(mx_tiles(g.m, 128) * tiles_n * splits));
+    cfg.blockDim = dim3(192);
+    cfg.dynamicSmemBytes = Small<kBN>::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim = {(unsigned)splits, 1, 1};
+    cfg.attrs = &at;
+    cfg.numAttrs = splits > 1;
+    cudaLaunchKernelEx(&cfg, kernel, g, splits, tiles_n);
+}
+
+template <typename T>
+void launch_pairs(const MatmulArgs &g, int sms, cudaStream_t s)
+{
+    static SmemLimit limit;
+    if (limit.ensure(matmul_pair_kernel<T>, kPairSmem) != cudaSuccess) return;       // the caller reports it
+    const long long tiles = mx_tiles(g.m, 256) * mx_tiles(g.n, 256), pairs = tiles < sms / 2 ? tiles : sms / 2;
+    matmul_pair_kernel<T><<<(unsigned)(2 * pairs), kPairThreads, kPairSmem, s>>>(g, tiles);
 }
 
 zoa_status check_matrix(const char *me, const char *name, const void *p)
@@ -549,19 +683,12 @@ extern "C" zoa_status zoa_mx4_matmul(const void *a, const void *b, size_t m, siz
     if (!g.limit.error_word) return ops_fail(ZOA_ERR_CUDA, "%s: no usable current device", me);
     const int sms = ops_sm_count();
     if (sms < 2) return ops_fail(ZOA_ERR_CUDA, "%s: no usable current device", me);
-    const long long pair_tiles = mx_tiles(g.m, 256) * mx_tiles(g.n, 256);
+    const ProductPlan plan = product_plan(g, sms);
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        if (pair_tiles >= sms / 2) {
-            static SmemLimit limit;
-            if (limit.ensure(matmul_pair_kernel<T>, kPairSmem) != cudaSuccess) return;
-            const long long pairs = pair_tiles < sms / 2 ? pair_tiles : sms / 2;
-            matmul_pair_kernel<T><<<(unsigned)(2 * pairs), kPairThreads, kPairSmem, s>>>(g, pair_tiles);
-            return;
-        }
-        static SmemLimit limit;
-        if (limit.ensure(matmul_kernel<T>, kMatmulSmem) != cudaSuccess) return;
-        matmul_kernel<T><<<dim3((unsigned)mx_tiles(g.m, 128), (unsigned)mx_tiles(g.n, 128)), 192, kMatmulSmem, s>>>(g);
+        if (plan.columns == 256) launch_pairs<T>(g, sms, s);
+        else if (plan.columns == 128) launch_small<T, 128>(g, plan.splits, s);
+        else launch_small<T, 64>(g, plan.splits, s);
     });
     return ops_launched(me);
 }
