@@ -14,7 +14,7 @@ HEADERS = ["zoa_device.cuh", "zoa_internal.h", "zoa_ring.cuh", "zoa_ops.h", "zoa
 # and no contraction of a multiply and an add into one fused operation.
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--fmad=false", "--ftz=false", "--prec-div=true", "--prec-sqrt=true",
-              "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall"] + os.environ.get("ZTUNE", "").split()
+              "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall"]
 
 
 def _stale() -> bool:

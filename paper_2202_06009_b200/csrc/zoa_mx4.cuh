@@ -17,6 +17,8 @@
 
 #include "zoa_ops.h"
 
+#include <type_traits>
+
 namespace zoa {
 
 constexpr int kMxTileRows = 128, kMxTileCols = 256, kMxBlock = 32;
@@ -59,6 +61,114 @@ __device__ __forceinline__ uint32_t mx_codes8(const uint64_t *p)
         : "=r"(out)
         : "l"(p[0]), "l"(p[1]), "l"(p[2]), "l"(p[3]));
     return out;
+}
+
+// Eight neighbours of a row as they lie in memory.
+template <typename T>
+struct Raw8 {
+    static constexpr int kWords = 2 * (int)sizeof(T);
+    uint32_t w[kWords];
+};
+
+// `have` of the eight exist (0 or less: none); the others are 0.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T *at, long long have, bool vec)
+{
+    Raw8<T> r;
+    if (vec && have >= 8) {
+#pragma unroll
+        for (int k = 0; k < Raw8<T>::kWords; k += 4) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(at) + k / 4);
+            r.w[k] = v.x;
+            r.w[k + 1] = v.y;
+            r.w[k + 2] = v.z;
+            r.w[k + 3] = v.w;
+        }
+        return r;
+    }
+#pragma unroll
+    for (int k = 0; k < Raw8<T>::kWords; ++k) {
+        if constexpr (sizeof(T) == 4) {
+            r.w[k] = k < have ? reinterpret_cast<const uint32_t *>(at)[k] : 0u;
+        } else {
+            const uint16_t *p = reinterpret_cast<const uint16_t *>(at) + 2 * k;
+            r.w[k] = (2 * k < have ? p[0] : 0u) | (2 * k + 1 < have ? (uint32_t)p[1] << 16 : 0u);
+        }
+    }
+    return r;
+}
+
+// The larger of two magnitudes (of each half, for the 16-bit types); a NaN wins.  binary32 compares its bits, which
+// order finite < inf < NaN without their sign.
+template <typename T>
+__device__ __forceinline__ uint32_t larger(uint32_t magnitude, uint32_t w)
+{
+    if constexpr (sizeof(T) == 4) {
+        return max(magnitude, w & 0x7FFFFFFFu);
+    } else {
+        using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+        const T2 r = __hmax2_nan(*reinterpret_cast<const T2 *>(&magnitude), __habs2(*reinterpret_cast<const T2 *>(&w)));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    }
+}
+// Of the two halves of a word of a 16-bit type: bits of magnitudes order like the magnitudes.
+__device__ __forceinline__ uint32_t larger_half(uint32_t m) { return max(m & 0xFFFFu, m >> 16); }
+// The magnitude of one element (the low half word of the 16-bit types) as binary32.
+template <typename T>
+__device__ __forceinline__ float magnitude_f32(uint32_t m)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(m);
+    else {
+        float lo, hi;
+        unpack2<T>(m, lo, hi);
+        return lo;
+    }
+}
+
+__device__ __forceinline__ uint64_t times2(uint32_t lo, uint32_t hi, uint64_t by)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"((uint64_t)hi << 32 | lo), "l"(by));
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t codes8(const Raw8<T> &r, float inv)
+{
+    const uint64_t by = (uint64_t)__float_as_uint(inv) << 32 | __float_as_uint(inv);
+    uint64_t p[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (sizeof(T) == 4) {
+            p[k] = times2(r.w[2 * k], r.w[2 * k + 1], by);
+        } else {
+            float lo, hi;
+            unpack2<T>(r.w[k], lo, hi);
+            p[k] = times2(__float_as_uint(lo), __float_as_uint(hi), by);
+        }
+    }
+    return mx_codes8(p);
+}
+
+// Scale byte of the block that this lane shares with its three neighbours.
+template <typename T>
+__device__ __forceinline__ uint32_t block_scale(const Raw8<T> &r)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < Raw8<T>::kWords; ++k) m = larger<T>(m, r.w[k]);
+    if (sizeof(T) == 2) m = larger_half(m);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    return mx_scale_byte(magnitude_f32<T>(m));
+}
+
+// Eight codes as eight binary16, the lowest nibble first.
+__device__ __forceinline__ void mx_halves8(uint32_t codes, uint32_t *v)
+{
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+        : "r"(codes));
 }
 
 }  // namespace zoa

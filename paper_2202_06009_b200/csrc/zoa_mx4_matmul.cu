@@ -636,6 +636,162 @@ void launch_pairs(const MatmulArgs &g, int sms, cudaStream_t s)
     matmul_pair_kernel<T><<<(unsigned)(2 * pairs), kPairThreads, kPairSmem, s>>>(g, tiles);
 }
 
+// ---- few rows ------------------------------------------------------------------------------------------------
+// out = Q(x) b^T for up to four rows of x, as when tokens are generated one at a time: every block rounds x for itself
+// (a few thousand elements) into shared memory while its weights are on their way, and multiplies on the ordinary
+// cores.  The product's time is that of reading b once.  A lane takes a block of 32 columns of one row of b: its codes
+// are 16 bytes and become pairs of binary16, x's elements lie as binary16; eight products of elements (multiples of
+// 1/4, at most 36) add up to less than 2^11 quarters, so sums of eight are exact in binary16, those of a block in
+// binary32.
+constexpr int kFewRows = 4, kFewWarps = 8, kFewAhead = 4;
+constexpr int kFewSmem = 200 * 1024;
+
+// 2^(a + b - 254) by two factors, neither of which leaves binary32's range.
+__device__ __forceinline__ float times_scales(float v, uint32_t a, uint32_t b)
+{
+    if (a == 255u || b == 255u) return __uint_as_float(0x7FC00000u);
+    const int e = (int)(a + b) - 254, half = e >> 1;
+    return v * __uint_as_float((uint32_t)(half + 127) << 23) * __uint_as_float((uint32_t)(e - half + 127) << 23);
+}
+__device__ __forceinline__ void halves8(uint32_t codes, __half2 *v) { mx_halves8(codes, reinterpret_cast<uint32_t *>(v)); }
+
+template <typename T, int kRows>
+__global__ void __launch_bounds__(kFewWarps * 32) few_rows_kernel(const T *__restrict__ x, long long ldx, bool vec, const MatmulArgs g,
+                                                                  long long k_cols, int parts)
+{
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    __shared__ float part_s[kFewWarps][4][kRows];
+    // x: [row][k tile][piece of 8 elements of a block][block] of 16 bytes, so that the eight blocks a warp reads lie in
+    // different banks; then [row][k tile][block] scale bytes.
+    uint4 *x_s = reinterpret_cast<uint4 *>(smem_raw);
+    uint8_t *scale_s = smem_raw + (size_t)kRows * g.tiles_k * 512;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int group = warp / parts, part = warp % parts;              // which four rows of b; which of the k tiles
+    const int rows_b = kFewWarps / parts * 4;                         // rows of b a block takes at a time
+    // This lane's row of b and, kFewAhead at a time, the k tiles whose codes are on their way.
+    long long n_next = (long long)blockIdx.x * rows_b + group * 4 + (lane >> 3);
+    int t_next = part;
+    uint4 codes[kFewAhead];
+    uint32_t bytes[kFewAhead];
+    auto fetch = [&] {
+        const int r = (int)(n_next % kMxTileRows), block = (lane & 7) ^ (r & 7);
+        const uint8_t *tile = g.b + (n_next / kMxTileRows * g.tiles_k + t_next) * kMxTileBytes;
+        const uint8_t *codes_at = tile + kMxScaleBytes + r * 128 + (lane & 7) * 16, *scale_at = tile + mx_scale_at(r, block);
+#pragma unroll
+        for (int i = 0; i < kFewAhead; ++i) {
+            codes[i] = make_uint4(0, 0, 0, 0);
+            bytes[i] = 0;
+            if (n_next < g.n && t_next + i * parts < g.tiles_k) {
+                codes[i] = __ldg(reinterpret_cast<const uint4 *>(codes_at + (long long)(i * parts) * kMxTileBytes));
+                bytes[i] = __ldg(scale_at + (long long)(i * parts) * kMxTileBytes);
+            }
+        }
+        t_next += kFewAhead * parts;
+        if (t_next - part >= (g.tiles_k - part + parts - 1) / parts * parts) {
+            t_next = part;
+            n_next += (long long)gridDim.x * rows_b;
+        }
+    };
+    fetch();
+    // x: a warp takes a line of 256 columns, a lane 8 of them.
+    for (int line = warp; line < kRows * g.tiles_k; line += kFewWarps) {
+        const int row = line / g.tiles_k, t = line % g.tiles_k;
+        const long long c = (long long)t * kMxTileCols + lane * 8;
+        const Raw8<T> v = load8(x + row * ldx + c, row < g.m ? k_cols - c : 0, vec);
+        const uint32_t byte = block_scale(v), q = byte == 255u ? 0u : codes8(v, mx_inverse(byte));
+        __half2 e[4];
+        halves8(q, e);
+        x_s[line * 32 + (lane & 3) * 8 + (lane >> 2)] = *reinterpret_cast<const uint4 *>(e);
+        if ((lane & 3) == 0) scale_s[line * 8 + (lane >> 2)] = (uint8_t)byte;
+    }
+    __syncthreads();
+    for (long long first = (long long)blockIdx.x * rows_b; first < g.n; first += (long long)gridDim.x * rows_b) {
+        const int block = (lane & 7) ^ (int)((first + group * 4 + (lane >> 3)) & 7);
+        float sum[kRows] = {};
+        for (int t0 = part; t0 < g.tiles_k; t0 += kFewAhead * parts) {
+            uint4 now[kFewAhead];
+            uint32_t scale[kFewAhead];
+#pragma unroll
+            for (int i = 0; i < kFewAhead; ++i) {
+                now[i] = codes[i];
+                scale[i] = bytes[i];
+            }
+            fetch();
+#pragma unroll
+            for (int i = 0; i < kFewAhead; ++i) {
+                const int t = t0 + i * parts;
+                if (t >= g.tiles_k) break;
+                __half2 w[16];
+                halves8(now[i].x, w);
+                halves8(now[i].y, w + 4);
+                halves8(now[i].z, w + 8);
+                halves8(now[i].w, w + 12);
+#pragma unroll
+                for (int m = 0; m < kRows; ++m) {
+                    const uint4 *at = x_s + (m * g.tiles_k + t) * 32 + block;
+                    float s = 0.0f;
+#pragma unroll
+                    for (int p = 0; p < 4; p += 2) {          // sixteen elements: eight products in either half
+                        const uint4 a0 = at[p * 8], a1 = at[p * 8 + 8];
+                        const __half2 *e0 = reinterpret_cast<const __half2 *>(&a0), *e1 = reinterpret_cast<const __half2 *>(&a1);
+                        __half2 acc = __hmul2(w[4 * p], e0[0]);
+#pragma unroll
+                        for (int k = 1; k < 4; ++k) acc = __hfma2(w[4 * p + k], e0[k], acc);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc = __hfma2(w[4 * p + 4 + k], e1[k], acc);
+                        const float2 f = __half22float2(acc);
+                        s += f.x + f.y;
+                    }
+                    sum[m] += times_scales(s, scale[i], scale_s[(m * g.tiles_k + t) * 8 + block]);
+                }
+            }
+        }
+        __syncthreads();          // the last round's part_s has been read
+#pragma unroll
+        for (int m = 0; m < kRows; ++m) {
+            sum[m] += __shfl_xor_sync(0xffffffffu, sum[m], 1);
+            sum[m] += __shfl_xor_sync(0xffffffffu, sum[m], 2);
+            sum[m] += __shfl_xor_sync(0xffffffffu, sum[m], 4);
+            if ((lane & 7) == 0) part_s[warp][lane >> 3][m] = sum[m];
+        }
+        __syncthreads();
+        // One thread per row of b and row of x adds the parts, in order.
+        for (int i = threadIdx.x; i < rows_b * kRows; i += kFewWarps * 32) {
+            const int m = i / rows_b, rb = i % rows_b;
+            const long long at = first + rb;
+            if (m >= g.m || at >= g.n) continue;
+            float v = part_s[rb / 4 * parts][rb % 4][m];
+            for (int p = 1; p < parts; ++p) v += part_s[rb / 4 * parts + p][rb % 4][m];
+            static_cast<T *>(g.out)[m * g.ld + at] = from_f32<T>(v);
+        }
+    }
+}
+
+// Rows that few_rows_kernel is compiled for, or 0 where the tensor cores are as fast in two launches (measured on one
+// B200: 2 x 4096 x 4096 7.8 us here, 9.3 there; 1 x 8192 x 8192 13.2 and 11.2; 4 x 6400 x 1600 8.1 and 8.1) or x is too
+// large for a block's shared memory.
+int few_rows(size_t m, size_t n, size_t k)
+{
+    const int rows = m <= 1 ? 1 : m <= 2 ? 2 : kFewRows;
+    const bool small = m <= (size_t)kFewRows && n <= kMxMaxSide && k <= kMxMaxSide && (double)m * (double)n * (double)k <= (double)(1 << 25);
+    return small && (size_t)mx_tiles((long long)k, kMxTileCols) * rows * 520 <= (size_t)kFewSmem ? rows : 0;
+}
+
+template <typename T, int kRows>
+void launch_few(const void *x, long long ldx, bool vec, const MatmulArgs &g, long long k, int sms, cudaStream_t s)
+{
+    static SmemLimit limit;
+    auto kernel = few_rows_kernel<T, kRows>;
+    if (limit.ensure(kernel, kFewSmem) != cudaSuccess) return;       // the caller reports it
+    // Warps that share rows of b divide its k tiles between them: more of them while there are fewer than two blocks
+    // an SM and every warp keeps two tiles.  No more blocks than the SMs hold: each rounds x once.
+    int parts = 1;
+    while (parts < kFewWarps && mx_tiles(g.n, 4 * kFewWarps / parts) < 2 * sms && g.tiles_k >= 4 * parts) parts *= 2;
+    const long long blocks = mx_tiles(g.n, 4 * kFewWarps / parts), most = (kRows == 1 ? 3ll : 2ll) * sms;
+    kernel<<<(unsigned)(blocks < most ? blocks : most), kFewWarps * 32, (size_t)kRows * g.tiles_k * 520, s>>>(static_cast<const T *>(x), ldx, vec, g,
+                                                                                                            k, parts);
+}
+
 zoa_status check_matrix(const char *me, const char *name, const void *p)
 {
     if (!p) return ops_fail(ZOA_ERR_ARG, "%s: %s is NULL", me, name);
@@ -695,16 +851,45 @@ extern "C" zoa_status zoa_mx4_matmul(const void *a, const void *b, size_t m, siz
 
 extern "C" size_t zoa_mx4_linear_work(size_t m, size_t n, size_t k)
 {
-    (void)n;
-    return zoa_mx4_size(m, k);
+    return few_rows(m, n, k) ? 0 : zoa_mx4_size(m, k);
 }
 
 extern "C" zoa_status zoa_mx4_linear(const void *x, int dtype, size_t m, size_t k, size_t ldx, const void *b, size_t n, void *out,
                                      size_t ld, void *work, void *stream)
 {
-    if (m && n && k && zoa_mx4_linear_work(m, n, k) && !work) return ops_fail(ZOA_ERR_ARG, "zoa_mx4_linear: work is NULL");
-    const zoa_status st = zoa_mx4_quantize(x, dtype, m, k, ldx, work, nullptr, stream);
-    return st != ZOA_OK ? st : zoa_mx4_matmul(work, b, m, n, k, out, dtype, ld, stream);
+    const char *me = "zoa_mx4_linear";
+    const int rows = few_rows(m, n, k);
+    if (!rows || !m || !n || !k) {
+        if (m && n && k && !work) return ops_fail(ZOA_ERR_ARG, "%s: work is NULL", me);
+        const zoa_status st = zoa_mx4_quantize(x, dtype, m, k, ldx, work, nullptr, stream);
+        return st != ZOA_OK ? st : zoa_mx4_matmul(work, b, m, n, k, out, dtype, ld, stream);
+    }
+    if (!dtype_ok(dtype)) return ops_fail(ZOA_ERR_ARG, "%s: unknown element type %d", me, dtype);
+    if (n > kMxMaxSide || k > kMxMaxSide) return ops_fail(ZOA_ERR_ARG, "%s: n and k must be at most 2^30", me);
+    if (!x || !out) return ops_fail(ZOA_ERR_ARG, "%s: a NULL pointer", me);
+    if (ldx < k || ld < n) return ops_fail(ZOA_ERR_ARG, "%s: ldx must be at least k and ld at least n", me);
+    if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) % dtype_bytes(dtype))
+        return ops_fail(ZOA_ERR_ARG, "%s: x or out is not aligned to its element type", me);
+    const zoa_status st = check_matrix(me, "b", b);
+    if (st != ZOA_OK) return st;
+    const int sms = ops_sm_count();
+    if (sms < 2) return ops_fail(ZOA_ERR_CUDA, "%s: no usable current device", me);
+    MatmulArgs g{};
+    g.b = static_cast<const uint8_t *>(b);
+    g.out = out;
+    g.m = (long long)m;
+    g.n = (long long)n;
+    g.ld = (long long)ld;
+    g.tiles_k = (int)mx_tiles((long long)k, kMxTileCols);
+    const bool vec = aligned16(x) && ldx * dtype_bytes(dtype) % 16 == 0;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        if (rows == 1) launch_few<T, 1>(x, (long long)ldx, vec, g, (long long)k, sms, s);
+        else if (rows == 2) launch_few<T, 2>(x, (long long)ldx, vec, g, (long long)k, sms, s);
+        else launch_few<T, kFewRows>(x, (long long)ldx, vec, g, (long long)k, sms, s);
+    });
+    return ops_launched(me);
 }
 
 extern "C" zoa_status zoa_mx4_linear_forward(const void *x, int x_type, size_t ldx, const void *w, int w_type, size_t ldw, size_t m,

@@ -1,99 +1,11 @@
 // Rounding to 4-bit microscaled form (along the rows, along the columns, or both from one read) and reading back.
 #include "zoa_mx4.cuh"
 
-#include <type_traits>
-
 namespace zoa {
 namespace {
 
 constexpr int kRowWarps = 8;      // warps of a block of quantize_rows_kernel
 constexpr int kRowsPerWarp = 4;   // rows whose loads a warp has in flight at once
-
-// Eight neighbours of a row as they lie in memory.
-template <typename T>
-struct Raw8 {
-    static constexpr int kWords = 2 * (int)sizeof(T);
-    uint32_t w[kWords];
-};
-
-// `have` of the eight exist (0 or less: none); the others are 0.
-template <typename T>
-__device__ __forceinline__ Raw8<T> load8(const T *at, long long have, bool vec)
-{
-    Raw8<T> r;
-    if (vec && have >= 8) {
-#pragma unroll
-        for (int k = 0; k < Raw8<T>::kWords; k += 4) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(at) + k / 4);
-            r.w[k] = v.x;
-            r.w[k + 1] = v.y;
-            r.w[k + 2] = v.z;
-            r.w[k + 3] = v.w;
-        }
-        return r;
-    }
-#pragma unroll
-    for (int k = 0; k < Raw8<T>::kWords; ++k) {
-        if constexpr (sizeof(T) == 4) {
-            r.w[k] = k < have ? reinterpret_cast<const uint32_t *>(at)[k] : 0u;
-        } else {
-            const uint16_t *p = reinterpret_cast<const uint16_t *>(at) + 2 * k;
-            r.w[k] = (2 * k < have ? p[0] : 0u) | (2 * k + 1 < have ? (uint32_t)p[1] << 16 : 0u);
-        }
-    }
-    return r;
-}
-
-// The larger of two magnitudes (of each half, for the 16-bit types); a NaN wins.  binary32 compares its bits, which
-// order finite < inf < NaN without their sign.
-template <typename T>
-__device__ __forceinline__ uint32_t larger(uint32_t magnitude, uint32_t w)
-{
-    if constexpr (sizeof(T) == 4) {
-        return max(magnitude, w & 0x7FFFFFFFu);
-    } else {
-        using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
-        const T2 r = __hmax2_nan(*reinterpret_cast<const T2 *>(&magnitude), __habs2(*reinterpret_cast<const T2 *>(&w)));
-        return *reinterpret_cast<const uint32_t *>(&r);
-    }
-}
-// Of the two halves of a word of a 16-bit type: bits of magnitudes order like the magnitudes.
-__device__ __forceinline__ uint32_t larger_half(uint32_t m) { return max(m & 0xFFFFu, m >> 16); }
-// The magnitude of one element (the low half word of the 16-bit types) as binary32.
-template <typename T>
-__device__ __forceinline__ float magnitude_f32(uint32_t m)
-{
-    if constexpr (sizeof(T) == 4) return __uint_as_float(m);
-    else {
-        float lo, hi;
-        unpack2<T>(m, lo, hi);
-        return lo;
-    }
-}
-
-__device__ __forceinline__ uint64_t times2(uint32_t lo, uint32_t hi, uint64_t by)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"((uint64_t)hi << 32 | lo), "l"(by));
-    return r;
-}
-template <typename T>
-__device__ __forceinline__ uint32_t codes8(const Raw8<T> &r, float inv)
-{
-    const uint64_t by = (uint64_t)__float_as_uint(inv) << 32 | __float_as_uint(inv);
-    uint64_t p[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if constexpr (sizeof(T) == 4) {
-            p[k] = times2(r.w[2 * k], r.w[2 * k + 1], by);
-        } else {
-            float lo, hi;
-            unpack2<T>(r.w[k], lo, hi);
-            p[k] = times2(__float_as_uint(lo), __float_as_uint(hi), by);
-        }
-    }
-    return mx_codes8(p);
-}
 
 // The 4-byte scale words of a row's two groups of 128 columns, from the scale byte that every lane of block
 // lane / 4 holds: complete in lanes 0 and 16.
@@ -103,19 +15,6 @@ __device__ __forceinline__ uint32_t gather_scales(uint32_t byte, int lane)
     w |= __shfl_xor_sync(0xffffffffu, w, 4);
     w |= __shfl_xor_sync(0xffffffffu, w, 8);
     return w;
-}
-
-// Scale byte of the block that this lane shares with its three neighbours.
-template <typename T>
-__device__ __forceinline__ uint32_t block_scale(const Raw8<T> &r)
-{
-    uint32_t m = 0;
-#pragma unroll
-    for (int k = 0; k < Raw8<T>::kWords; ++k) m = larger<T>(m, r.w[k]);
-    if (sizeof(T) == 2) m = larger_half(m);
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    return mx_scale_byte(magnitude_f32<T>(m));
 }
 
 // One warp takes 256 columns (a line of a tile) of kRowsPerWarp rows at a time, a lane 8 neighbours: a block is four
@@ -193,25 +92,50 @@ __global__ void __launch_bounds__(kBothThreads) quantize_both_kernel(const T *__
     uint8_t *tile = out ? out + ((r0 / kMxTileRows) * tiles_c + c0 / kMxTileCols) * kMxTileBytes : nullptr;
     const bool last_half = group == 0 && c0 + kBothSide >= cols;        // the tile's second half has no block of its own
 
-    // A half warp holds 128 columns of a row; all loads first.
+    // A half warp holds 128 columns of a row; all loads first.  Rows that are not aligned go element by element to
+    // shared memory, where they are.
     Raw8<T> v[kPasses];
+    auto word_at = [&](int rr, int k) { return tile_s + rr * kRowWords + ((l16 * Raw8<T>::kWords + k) ^ ((rr >> 5) * 8)); };
+    if (vec) {
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-        const int rr = i * 16 + warp * 2 + half;
-        if (r0 + rr < rows) {
-            v[i] = load8(x + (r0 + rr) * ld + c0 + l16 * 8, cols - c0 - l16 * 8, vec);
-        } else {
+        for (int i = 0; i < kPasses; ++i) {
+            const int rr = i * 16 + warp * 2 + half;
+            v[i] = load8(x + (r0 + rr) * ld + c0 + l16 * 8, r0 + rr < rows ? cols - c0 - l16 * 8 : 0, true);
+        }
+    } else {
+        using Bits = typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type;
+        const int col = threadIdx.x % kBothSide;
+#pragma unroll 8
+        for (int i = 0; i < kBothSide / 2; ++i) {
+            const int rr = i * 2 + threadIdx.x / kBothSide;
+            Bits e = 0;
+            if (r0 + rr < rows && c0 + col < cols) e = reinterpret_cast<const Bits *>(x)[(r0 + rr) * ld + c0 + col];
+            const int word = sizeof(T) == 4 ? col : col >> 1;
+            Bits *at = reinterpret_cast<Bits *>(tile_s + rr * kRowWords + (word ^ ((rr >> 5) * 8)));
+            at[sizeof(T) == 4 ? 0 : col & 1] = e;
+        }
+        __syncthreads();
 #pragma unroll
-            for (int k = 0; k < Raw8<T>::kWords; ++k) v[i].w[k] = 0u;
+        for (int i = 0; i < kPasses; ++i) {
+            const int rr = i * 16 + warp * 2 + half;
+#pragma unroll
+            for (int k = 0; k < Raw8<T>::kWords; k += 4) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(word_at(rr, k));
+                v[i].w[k] = w.x;
+                v[i].w[k + 1] = w.y;
+                v[i].w[k + 2] = w.z;
+                v[i].w[k + 3] = w.w;
+            }
         }
     }
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
         const int rr = i * 16 + warp * 2 + half;
+        if (vec) {
 #pragma unroll
-        for (int k = 0; k < Raw8<T>::kWords; k += 4)
-            *reinterpret_cast<uint4 *>(tile_s + rr * kRowWords + ((l16 * Raw8<T>::kWords + k) ^ ((rr >> 5) * 8))) =
-                make_uint4(v[i].w[k], v[i].w[k + 1], v[i].w[k + 2], v[i].w[k + 3]);
+            for (int k = 0; k < Raw8<T>::kWords; k += 4)
+                *reinterpret_cast<uint4 *>(word_at(rr, k)) = make_uint4(v[i].w[k], v[i].w[k + 1], v[i].w[k + 2], v[i].w[k + 3]);
+        }
         if (!tile) continue;
         const uint32_t byte = block_scale(v[i]);
         const uint32_t codes = byte == 255u ? 0u : codes8(v[i], mx_inverse(byte));
@@ -343,14 +267,12 @@ __global__ void __launch_bounds__(kRowWarps * 32) dequantize_kernel(const uint8_
         }
         const float s = mx_scale(bytes[i]);
         float v[8];
+        uint32_t h[4];
+        mx_halves8(codes[i], h);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            uint32_t h2;
-            asm("{\n\t.reg .b8 lo, hi;\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tmov.b16 {lo, hi}, t;\n\tcvt.rn.f16x2.e2m1x2 %0, lo;\n\t}"
-                : "=r"(h2)
-                : "r"(codes[i] >> (8 * k)));
             float lo, hi;
-            unpack2<__half>(h2, lo, hi);
+            unpack2<__half>(h[k], lo, hi);
             v[2 * k] = lo * s;
             v[2 * k + 1] = hi * s;
         }
