@@ -141,9 +141,12 @@ struct Pairs {
     }
     using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
     static __device__ __forceinline__ T2 as2(uint32_t w) { return *reinterpret_cast<const T2 *>(&w); }
-    static __device__ __forceinline__ float largest(const uint4 &w)
+    // The largest elements of several vectors, joined as they lie, and taken apart once.
+    using Max = T2;
+    static __device__ __forceinline__ Max largest(const uint4 &w) { return __hmax2(__hmax2(as2(w.x), as2(w.y)), __hmax2(as2(w.z), as2(w.w))); }
+    static __device__ __forceinline__ Max larger(Max a, Max b) { return __hmax2(a, b); }
+    static __device__ __forceinline__ float value(Max m)
     {
-        const T2 m = __hmax2(__hmax2(as2(w.x), as2(w.y)), __hmax2(as2(w.z), as2(w.w)));
         float lo, hi;
         unpack2<T>(*reinterpret_cast<const uint32_t *>(&m), lo, hi);
         return fmaxf(lo, hi);
@@ -161,10 +164,13 @@ struct Pairs<float> {
     {
         return make_uint4((uint32_t)x[0], (uint32_t)(x[0] >> 32), (uint32_t)x[1], (uint32_t)(x[1] >> 32));
     }
-    static __device__ __forceinline__ float largest(const uint4 &w)
+    using Max = float;
+    static __device__ __forceinline__ Max largest(const uint4 &w)
     {
         return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
     }
+    static __device__ __forceinline__ Max larger(Max a, Max b) { return fmaxf(a, b); }
+    static __device__ __forceinline__ float value(Max m) { return m; }
 };
 
 template <typename T> constexpr uint32_t kMinusInfBits = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00u : 0xFF80u;
@@ -188,17 +194,18 @@ struct RowCut {
 // One entry of a row's list.
 struct Entry {
     int token;       // -1: skipped
-    float z;         // the student's logit; NaN bits never matter here
+    float z;         // the student's logit
     float p;         // the teacher's logit, then its probability
+    int first;       // this block's token, and its first entry
 };
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 8;
-constexpr int kBatch = 4;          // vectors a thread has in flight
-constexpr int kBlocksPerSm = 4;
+constexpr int kMaxCluster = 8, kMaxWarps = 8;
+constexpr int kBatch = 4;                 // vectors a thread has in flight
+constexpr int kThreadsPerSm = 1024;       // what 64 registers a thread leave room for
 
 struct DistillShared {
     unsigned long long exchange;
-    Sums part[kWarps];
+    Sums part[kMaxWarps];
     Sums theirs[kMaxCluster];
     float mass, soft;
     int any, twice, gave_up;
@@ -207,16 +214,21 @@ struct DistillShared {
 // A cluster of `blocks` blocks takes a row, each block a slice of it: one for many rows, up to eight for few.  Pass 1
 // reads the row for its sums, pass 2 reads it again (from L2: the rows in flight fit there) and writes the gradient.
 // Several blocks share an SM, so that one row's fixed costs - the list's dependent loads, the joins, the coefficients -
-// run beside other rows' sums.  The listed tokens enter the sums from the list, so that the sum over the rest costs a
-// byte of the bitmap per vector and never a difference of two large sums.
+// run beside other rows' sums.  The sum over the unlisted tokens is the whole sum less the listed ones, where that is at
+// least a 64th of the whole (its rounding error is then below 64 times that of a sum); other rows are summed again with
+// the listed tokens left out by a bitmap, as rows split over a cluster always are.
 //
 // What bounds it, apart from device memory: exponentials, one per element and pass.  exp(z - m) is the square of
 // exp((z - m) / 2), so at temperature 2 the hard part needs none of its own (kPower 2), at temperature 1 it is the
 // soft part's (kPower 0, also where there is no hard part); other temperatures pay for both (kPower -1).
-template <typename T, int kPower>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const DistillArgs a, const int blocks, const WaitLimit limit)
+//
+// Threads a row: 128 for the loss alone, where more rows in flight hide more (8192 x 50257: 151 us, 256 threads 172);
+// 256 with a gradient, where more rows in flight no longer fit L2 between the passes (334 us, 128 threads 404).
+template <typename T, int kPower, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_kernel(const DistillArgs a, const int blocks,
+                                                                                     const WaitLimit limit)
 {
-    constexpr int E = Vec<T>::kElems, P = Pairs<T>::kCount;
+    constexpr int E = Vec<T>::kElems, P = Pairs<T>::kCount, kWarps = kThreads / 32;
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ DistillShared sh;
     Entry *list = reinterpret_cast<Entry *>(smem_raw);                                   // [top]
@@ -242,15 +254,36 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
     // pass is asked for before the fixed costs that come ahead of it.
     const uint4 *vectors = reinterpret_cast<const uint4 *>(z + cut.head);
     constexpr uint32_t kNone = sizeof(T) == 4 ? kMinusInfBits<T> : kMinusInfBits<T> * 0x10001u;
-    uint4 word[kBatch], ahead[kBatch];
-    auto fetch = [&](int q) {
+    constexpr int kStep = kBatch * kThreads;
+    const int whole = (q1 - q0) / kStep, batches = (q1 - q0 + kStep - 1) / kStep;       // batches that are whole for all threads; all
+    const int last = (q1 - q0 - whole * kStep + kThreads - 1) / kThreads;               // vectors a thread has in a batch that is not, at most
+    uint4 ahead[kBatch];          // the batch that is on its way
+    auto fetch = [&](int i) {
+        const int q = q0 + i * kStep + tid;
+        if (i < whole) {
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) ahead[k] = q + k * kThreads < q1 ? vectors[q + k * kThreads] : make_uint4(kNone, kNone, kNone, kNone);
+            for (int k = 0; k < kBatch; ++k) ahead[k] = vectors[q + k * kThreads];
+        } else if (i < batches) {
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) ahead[k] = q + k * kThreads < q1 ? vectors[q + k * kThreads] : make_uint4(kNone, kNone, kNone, kNone);
+        }
+    };
+    // f(batch, number) for every batch of the row, the next one on its way; the first has been fetched.  (Two batches by
+    // turns would save the copies, but the longer loops miss the instruction cache: 334 -> 366 us for 8192 x 50257.)
+    auto each_batch = [&](auto f) {
+#pragma unroll 1
+        for (int i = 0; i < batches; ++i) {
+            uint4 word[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) word[k] = ahead[k];
+            fetch(i + 1);
+            f(word, i);
+        }
     };
 
     float w = a.weight ? a.weight[row] : 1.0f;
     if (a.grad_loss) w *= a.grad_loss[row];
-    fetch(q0 + tid);
+    if (blocks == 1 || a.stats_in) fetch(0);
     if (w == 0.0f) {        // nothing of the row is looked at
         if (grad) {
             const RowCut<T> g(grad, a.vocab);
@@ -278,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
     for (int k = tid; k < a.top; k += kThreads) {
         const int i = a.index[row * a.top + k];
         const bool ok = i >= 0 && i < a.vocab;
-        list[k] = Entry{ok ? i : -1, ok ? to_f32(z[i]) : 0.0f, to_f32(static_cast<const T *>(a.teacher)[row * a.top + k])};
+        list[k] = Entry{ok ? i : -1, ok ? to_f32(z[i]) : 0.0f, to_f32(static_cast<const T *>(a.teacher)[row * a.top + k]), 0};
     }
     const int label = a.labels ? a.labels[row] : -1;
     const bool hard = label >= 0 && label < a.vocab;
@@ -287,17 +320,12 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
     // From here on other blocks may replace their slices of the row by gradients, once they have waited for this.
     if (blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 
-    Sums t{-INFINITY, 0.0f, 0.0f, 0.0f};
     for (int k = tid; k < a.top; k += kThreads) {
         const int i = list[k].token;
         if (i < 0) continue;
         const uint32_t bit = 1u << ((i + cut.shift) & 31);
-        if (atomicOr(&bits[(i + cut.shift) >> 5], bit) & bit) {
-            sh.twice = 1;
-        } else if (!a.stats_in && mine(i)) {       // the listed tokens' share of the sums, each token once
-            const float x = list[k].z, one = x == -INFINITY ? 0.0f : 1.0f + 0.0f * x;      // NaN for +inf and NaN
-            t = join(t, Sums{x, one, one, 0.0f}, c);
-        }
+        if (atomicOr(&bits[(i + cut.shift) >> 5], bit) & bit) sh.twice = 1;
+        else list[k].first = mine(i);
     }
     __syncthreads();
     if (warp == kWarps - 1) {          // the teacher's probabilities, by one warp beside the others' sums
@@ -337,13 +365,24 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
     }
 
     // The student's sums.
+    Sums t;
     if (a.stats_in) {
         const float4 s4 = reinterpret_cast<const float4 *>(a.stats_in)[row];
         t = Sums{s4.x, s4.y, s4.z, s4.w};
         __syncthreads();
-    } else {
-        uint64_t minus_m = pair(-base_of(t.m), -base_of(t.m)), s2 = pair(0.0f, 0.0f), f2 = s2;
+    }
+    for (bool masked = blocks > 1; !a.stats_in;) {
+        // The list's share: where its tokens are left out of the row's sums they are added here, else they are taken from
+        // the sum over the rest; each token once.
+        t = Sums{-INFINITY, 0.0f, 0.0f, 0.0f};
+        if (masked || a.lse)
+            for (int k = tid; k < a.top; k += kThreads) {
+                if (!list[k].first) continue;
+                const float x = list[k].z, one = x == -INFINITY ? 0.0f : 1.0f + 0.0f * x;      // NaN for +inf and NaN
+                t = join(t, masked ? Sums{x, one, one, 0.0f} : Sums{x, 0.0f, 0.0f, -one}, c);
+            }
         float m = t.m;
+        uint64_t minus_m = pair(-base_of(m), -base_of(m)), s2 = pair(0.0f, 0.0f), f2 = s2;
         const uint64_t c2 = pair(c, c), l2 = pair(kLog2e, kLog2e);
         // The base need not be the maximum itself: powers up to 2^40 above it lose nothing in binary32, and the sums are
         // rebased for a logit further above alone (else nearly every vector would, for one lane or other).
@@ -354,6 +393,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
                 s2 = mul2(s2, pair(f, f));
                 f2 = mul2(f2, pair(f1, f1));
                 t.s *= f;
+                t.r *= f;
                 t.s1 *= f1;
                 m = vm;
                 minus_m = pair(-m, -m);
@@ -370,10 +410,10 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
                 if (kPower == -1) f2 = add2(f2, ex2_2(mul2(d, l2)));
             }
         };
-        const uint8_t *vector_bits = reinterpret_cast<const uint8_t *>(bits) ;
+        const uint8_t *vector_bits = reinterpret_cast<const uint8_t *>(bits);
         const int first_bit = cut.head + cut.shift;          // a multiple of E
-        auto without_listed = [&](uint4 word, int q) {       // listed elements as -inf
-            uint32_t in = E == 8 ? vector_bits[(first_bit >> 3) + q] : vector_bits[(first_bit + q * E) >> 3] >> ((first_bit + q * E) & 7) & 15u;
+        auto without_listed = [&](uint4 &word, int q) {       // listed elements as -inf
+            const uint32_t in = E == 8 ? vector_bits[(first_bit >> 3) + q] : vector_bits[(first_bit + q * E) >> 3] >> ((first_bit + q * E) & 7) & 15u;
             if (in) {
                 uint32_t *x = &word.x;
 #pragma unroll
@@ -383,44 +423,51 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
                         else x[k >> 1] = k & 1 ? (x[k >> 1] & 0xFFFFu) | (kNone & 0xFFFF0000u) : (x[k >> 1] & 0xFFFF0000u) | (kNone & 0xFFFFu);
                     }
             }
-            return word;
         };
-        for (int q = q0 + tid; q < q1; q += kBatch * kThreads) {
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) word[k] = ahead[k];
-            fetch(q + kBatch * kThreads);
-            float vm = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                if (q + k * kThreads < q1) word[k] = without_listed(word[k], q + k * kThreads);
-                vm = fmaxf(vm, Pairs<T>::largest(word[k]));
+        if (masked) {
+#pragma unroll 1
+            for (int q = q0 + tid; q < q1; q += kThreads) {
+                uint4 word = vectors[q];
+                without_listed(word, q);
+                rebase(Pairs<T>::value(Pairs<T>::largest(word)));
+                take(word);
             }
-            rebase(vm);
+        } else {
+            each_batch([&](const uint4 (&word)[kBatch], int i) {
+                auto vm = Pairs<T>::largest(word[0]);
 #pragma unroll
-            for (int k = 0; k < kBatch; ++k)
-                if (k == 0 || q + k * kThreads < q1) take(word[k]);
+                for (int k = 1; k < kBatch; ++k) vm = Pairs<T>::larger(vm, Pairs<T>::largest(word[k]));
+                rebase(Pairs<T>::value(vm));
+                const int n = i < whole ? kBatch : last;
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k)
+                    if (k < n) take(word[k]);
+            });
         }
-        if (tid < singles && !(listed_bits(single) & 1)) {
-            const float x = to_f32(z[single]), b = base_of(fmaxf(m, x));
-            const float f = x > m ? ex2((m - b) * c) : 1.0f, f1 = x > m ? ex2((m - b) * kLog2e) : 1.0f;
-            s2 = add2(mul2(s2, pair(f, f)), pair(ex2((x - b) * c), 0.0f));
-            f2 = add2(mul2(f2, pair(f1, f1)), pair(ex2((x - b) * kLog2e), 0.0f));
-            t.s *= f;
-            t.s1 *= f1;
-            m = fmaxf(m, x);
+        if (tid < singles && !(masked && listed_bits(single) & 1)) {
+            const float x = to_f32(z[single]);
+            rebase(x);
+            const float d = x - base_of(m);
+            s2 = add2(s2, pair(ex2(d * c), 0.0f));
+            f2 = add2(f2, pair(ex2(d * kLog2e), 0.0f));
         }
-        if (grad) fetch(q0 + tid);
+        if (grad) fetch(0);
         float lo, hi;
         unpair(s2, lo, hi);
         t.m = m;
-        t.r = lo + hi;
-        t.s += t.r;
+        t.r += lo + hi;
+        t.s += lo + hi;
         unpair(f2, lo, hi);
         t.s1 = kPower == 0 ? t.s : t.s1 + (lo + hi);
         t = warp_join(t, c);
         if (lane == 0) sh.part[warp] = t;
         __syncthreads();
         t = warp_join(lane < kWarps ? sh.part[lane] : Sums{-INFINITY, 0.0f, 0.0f, 0.0f}, c);
+        if (!masked && a.lse && t.r < t.s * 0.015625f) {
+            masked = true;
+            __syncthreads();          // all have read the parts
+            continue;
+        }
         if (blocks > 1) {      // every block tells every block
             asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
             const uint32_t bar = smem_addr(&sh.exchange);
@@ -436,6 +483,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
         }
         t.m = base_of(t.m);
         if (a.stats && tid == 0 && rank == 0) reinterpret_cast<float4 *>(a.stats)[row] = make_float4(t.m, t.s, t.s1, t.r);
+        break;
     }
     if (blocks > 1) {          // nobody leaves before the others are done with its memory
         if (a.stats_in) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -469,13 +517,11 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
         const float cu_all = kPower == 0 ? cu + cb : cu;
         const uint64_t cu2 = pair(cu_all, cu_all), cb2 = pair(cb, cb);
         const bool same = ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0;
-        for (int q = q0 + tid; q < q1; q += kBatch * kThreads) {
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) word[k] = ahead[k];
-            fetch(q + kBatch * kThreads);
+        each_batch([&](const uint4 (&word)[kBatch], int i) {
+            const int q = q0 + i * kStep + tid;
 #pragma unroll
             for (int h = 0; h < kBatch; ++h) {
-                if (q + h * kThreads >= q1) break;
+                if (i >= whole && q + h * kThreads >= q1) break;
                 uint64_t x[P];
                 Pairs<T>::unpack(word[h], x);
 #pragma unroll
@@ -498,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
                     }
                 }
             }
-        }
+        });
         if (tid < singles) {
             const float d = to_f32(z[single]) - t.m;
             grad[single] = from_f32<T>(cu * ex2(d * c) + cb * ex2(d * kLog2e));
@@ -527,11 +573,11 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_kernel(const D
     if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <typename T, int kPower>
+template <typename T, int kPower, int kThreads>
 void launch_kernel(const DistillArgs &a, int blocks, const WaitLimit &wait_limit, cudaStream_t s)
 {
     static SmemLimit limit;
-    auto kernel = distill_kernel<T, kPower>;
+    auto kernel = distill_kernel<T, kPower, kThreads>;
     if (limit.ensure(kernel, (int)(kMaxTop * sizeof(Entry) + kMaxVocab / 8 + 64)) != cudaSuccess) return;     // the caller reports it
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(a.rows * blocks));
@@ -597,9 +643,16 @@ zoa_status launch(const char *me, const zoa_distill_args *x, const float *stats_
     if (a.rows * blocks > 0x7FFFFFFFll) return ops_fail(ZOA_ERR_ARG, "%s: at most 2^31 - 1 rows", me);
     with_type(x->dtype, [&](auto t) {
         using T = decltype(t);
-        if (a.temperature == 1.0f || !a.labels) launch_kernel<T, 0>(a, blocks, wait_limit, s);
-        else if (a.temperature == 2.0f) launch_kernel<T, 2>(a, blocks, wait_limit, s);
-        else launch_kernel<T, -1>(a, blocks, wait_limit, s);
+        const int power = a.temperature == 1.0f || !a.labels ? 0 : a.temperature == 2.0f ? 2 : -1;
+        if (!a.grad && blocks == 1) {
+            if (power == 0) launch_kernel<T, 0, 128>(a, blocks, wait_limit, s);
+            else if (power == 2) launch_kernel<T, 2, 128>(a, blocks, wait_limit, s);
+            else launch_kernel<T, -1, 128>(a, blocks, wait_limit, s);
+        } else {
+            if (power == 0) launch_kernel<T, 0, 256>(a, blocks, wait_limit, s);
+            else if (power == 2) launch_kernel<T, 2, 256>(a, blocks, wait_limit, s);
+            else launch_kernel<T, -1, 256>(a, blocks, wait_limit, s);
+        }
     });
     return ops_launched(me);
 }
