@@ -206,7 +206,7 @@ constexpr int kThreadsPerSm = 1024;       // what 64 registers a thread leave ro
 struct DistillShared {
     unsigned long long exchange;
     Sums part[kMaxWarps];
-    Sums theirs[kMaxCluster];
+    Sums theirs[2][kMaxCluster];
     float mass, soft;
     int any, twice, gave_up;
 };
@@ -216,7 +216,7 @@ struct DistillShared {
 // Several blocks share an SM, so that one row's fixed costs - the list's dependent loads, the joins, the coefficients -
 // run beside other rows' sums.  The sum over the unlisted tokens is the whole sum less the listed ones, where that is at
 // least a 64th of the whole (its rounding error is then below 64 times that of a sum); other rows are summed again with
-// the listed tokens left out by a bitmap, as rows split over a cluster always are.
+// the listed tokens left out by a bitmap.
 //
 // What bounds it, apart from device memory: exponentials, one per element and pass.  exp(z - m) is the square of
 // exp((z - m) / 2), so at temperature 2 the hard part needs none of its own (kPower 2), at temperature 1 it is the
@@ -224,10 +224,12 @@ struct DistillShared {
 //
 // Threads a row: 128 for the loss alone, where more rows in flight hide more (8192 x 50257: 151 us, 256 threads 172);
 // 256 with a gradient, where more rows in flight no longer fit L2 between the passes (334 us, 128 threads 404).
-template <typename T, int kPower, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_kernel(const DistillArgs a, const int blocks,
+// kAlone: one block a row.
+template <typename T, int kPower, int kThreads, bool kAlone>
+__global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_kernel(const DistillArgs a, const int cluster_blocks,
                                                                                      const WaitLimit limit)
 {
+    const int blocks = kAlone ? 1 : cluster_blocks;
     constexpr int E = Vec<T>::kElems, P = Pairs<T>::kCount, kWarps = kThreads / 32;
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ DistillShared sh;
@@ -283,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_ke
 
     float w = a.weight ? a.weight[row] : 1.0f;
     if (a.grad_loss) w *= a.grad_loss[row];
-    if (blocks == 1 || a.stats_in) fetch(0);
+    fetch(0);
     if (w == 0.0f) {        // nothing of the row is looked at
         if (grad) {
             const RowCut<T> g(grad, a.vocab);
@@ -371,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_ke
         t = Sums{s4.x, s4.y, s4.z, s4.w};
         __syncthreads();
     }
-    for (bool masked = blocks > 1; !a.stats_in;) {
+    for (int masked = 0; !a.stats_in; ++masked) {
         // The list's share: where its tokens are left out of the row's sums they are added here, else they are taken from
         // the sum over the rest; each token once.
         t = Sums{-INFINITY, 0.0f, 0.0f, 0.0f};
@@ -463,23 +465,22 @@ __global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_ke
         if (lane == 0) sh.part[warp] = t;
         __syncthreads();
         t = warp_join(lane < kWarps ? sh.part[lane] : Sums{-INFINITY, 0.0f, 0.0f, 0.0f}, c);
-        if (!masked && a.lse && t.r < t.s * 0.015625f) {
-            masked = true;
-            __syncthreads();          // all have read the parts
-            continue;
-        }
         if (blocks > 1) {      // every block tells every block
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            if (!masked) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
             const uint32_t bar = smem_addr(&sh.exchange);
             if (warp == 0 && lane < blocks) {
                 uint32_t remote;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_addr(&sh.theirs[rank])), "r"(lane));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_addr(&sh.theirs[masked][rank])), "r"(lane));
                 asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(remote), "f"(t.m), "f"(t.s), "f"(t.s1), "f"(t.r)
                              : "memory");
                 mbar_arrive_at(bar, (uint32_t)lane);
             }
-            mbar_wait<true>(bar, 0, &sh.gave_up, limit);
-            t = warp_join(lane < blocks ? sh.theirs[lane] : Sums{-INFINITY, 0.0f, 0.0f, 0.0f}, c);
+            mbar_wait<true>(bar, (uint32_t)masked, &sh.gave_up, limit);
+            t = warp_join(lane < blocks ? sh.theirs[masked][lane] : Sums{-INFINITY, 0.0f, 0.0f, 0.0f}, c);
+        }
+        if (!masked && a.lse && t.r < t.s * 0.015625f) {
+            __syncthreads();          // all have read the parts
+            continue;
         }
         t.m = base_of(t.m);
         if (a.stats && tid == 0 && rank == 0) reinterpret_cast<float4 *>(a.stats)[row] = make_float4(t.m, t.s, t.s1, t.r);
@@ -573,11 +574,11 @@ __global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_ke
     if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <typename T, int kPower, int kThreads>
+template <typename T, int kPower, int kThreads, bool kAlone>
 void launch_kernel(const DistillArgs &a, int blocks, const WaitLimit &wait_limit, cudaStream_t s)
 {
     static SmemLimit limit;
-    auto kernel = distill_kernel<T, kPower, kThreads>;
+    auto kernel = distill_kernel<T, kPower, kThreads, kAlone>;
     if (limit.ensure(kernel, (int)(kMaxTop * sizeof(Entry) + kMaxVocab / 8 + 64)) != cudaSuccess) return;     // the caller reports it
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(a.rows * blocks));
@@ -637,22 +638,22 @@ zoa_status launch(const char *me, const zoa_distill_args *x, const float *stats_
     const int sms = ops_sm_count();
     WaitLimit wait_limit{ops_error_word(), ops_wait_limit_ns()};
     if (sms < 1 || !wait_limit.error_word) return ops_fail(ZOA_ERR_CUDA, "%s: no usable current device", me);
-    // Blocks for a row: more while there are SMs without one and a slice stays above 4 KB.
+    // Blocks for a row: more while all of them fit the device at once (four to an SM) and a slice stays above 4 KB.
     int blocks = 1;
-    while (blocks < kMaxCluster && a.rows * blocks * 2 <= 2 * sms && (size_t)a.vocab * e / (blocks * 2) >= 4096) blocks *= 2;
+    while (blocks < kMaxCluster && a.rows * blocks * 2 <= 4 * sms && (size_t)a.vocab * e / (blocks * 2) >= 4096) blocks *= 2;
     if (a.rows * blocks > 0x7FFFFFFFll) return ops_fail(ZOA_ERR_ARG, "%s: at most 2^31 - 1 rows", me);
     with_type(x->dtype, [&](auto t) {
         using T = decltype(t);
         const int power = a.temperature == 1.0f || !a.labels ? 0 : a.temperature == 2.0f ? 2 : -1;
-        if (!a.grad && blocks == 1) {
-            if (power == 0) launch_kernel<T, 0, 128>(a, blocks, wait_limit, s);
-            else if (power == 2) launch_kernel<T, 2, 128>(a, blocks, wait_limit, s);
-            else launch_kernel<T, -1, 128>(a, blocks, wait_limit, s);
-        } else {
-            if (power == 0) launch_kernel<T, 0, 256>(a, blocks, wait_limit, s);
-            else if (power == 2) launch_kernel<T, 2, 256>(a, blocks, wait_limit, s);
-            else launch_kernel<T, -1, 256>(a, blocks, wait_limit, s);
-        }
+        auto go = [&](auto p) {
+            constexpr int kPower = decltype(p)::value;
+            if (blocks > 1) launch_kernel<T, kPower, 256, false>(a, blocks, wait_limit, s);
+            else if (a.grad) launch_kernel<T, kPower, 256, true>(a, 1, wait_limit, s);
+            else launch_kernel<T, kPower, 128, true>(a, 1, wait_limit, s);
+        };
+        if (power == 0) go(std::integral_constant<int, 0>{});
+        else if (power == 2) go(std::integral_constant<int, 2>{});
+        else go(std::integral_constant<int, -1>{});
     });
     return ops_launched(me);
 }
