@@ -149,6 +149,64 @@ __device__ __forceinline__ uint32_t codes8(const Raw8<T> &r, float inv)
     return mx_codes8(p);
 }
 
+// A whole block of a row, 32 elements, as they lie in memory.
+template <typename T>
+struct Raw32 {
+    static constexpr int kWords = 8 * (int)sizeof(T);
+    uint32_t w[kWords];
+    __device__ __forceinline__ Raw8<T> eight(int k) const
+    {
+        Raw8<T> r;
+#pragma unroll
+        for (int i = 0; i < Raw8<T>::kWords; ++i) r.w[i] = w[k * Raw8<T>::kWords + i];
+        return r;
+    }
+};
+template <typename T>
+__device__ __forceinline__ Raw32<T> load32(const T *at, long long have, bool vec)
+{
+    Raw32<T> r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const Raw8<T> e = load8(at + 8 * k, have - 8 * k, vec);
+#pragma unroll
+        for (int i = 0; i < Raw8<T>::kWords; ++i) r.w[k * Raw8<T>::kWords + i] = e.w[i];
+    }
+    return r;
+}
+// Its scale byte, and its codes.
+template <typename T>
+__device__ __forceinline__ uint4 round32_block(const Raw32<T> &r, uint32_t &byte)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < Raw32<T>::kWords; ++k) m = larger<T>(m, r.w[k]);
+    if (sizeof(T) == 2) m = larger_half(m);
+    byte = mx_scale_byte(magnitude_f32<T>(m));
+    if (byte == 255u) return make_uint4(0, 0, 0, 0);
+    const float inv = mx_inverse(byte);
+    return make_uint4(codes8(r.eight(0), inv), codes8(r.eight(1), inv), codes8(r.eight(2), inv), codes8(r.eight(3), inv));
+}
+// The scale word of four neighbouring blocks, one to a lane, lane & 3 being the block: complete in all four.
+__device__ __forceinline__ uint32_t scale_word(uint32_t byte, int lane)
+{
+    uint32_t w = byte << (8 * (lane & 3));
+    w |= __shfl_xor_sync(0xffffffffu, w, 1);
+    w |= __shfl_xor_sync(0xffffffffu, w, 2);
+    return w;
+}
+
+// A matrix to be rounded both ways (out may be NULL), and the launch for one or two of them (b.rows = 0: one).
+struct BothJob {
+    const void *x;
+    uint8_t *out, *out_t;
+    long long rows, cols, ld;
+    int vec;
+};
+zoa_status mx4_check_source(const char *me, const void *x, int dtype, size_t rows, size_t cols, size_t ld, const void *out, const void *out_t);
+BothJob mx4_both_job(const void *x, int dtype, size_t rows, size_t cols, size_t ld, void *out, void *out_t);
+zoa_status mx4_launch_both(const char *me, int dtype, const BothJob &a, const BothJob &b, cudaStream_t s);
+
 // Scale byte of the block that this lane shares with its three neighbours.
 template <typename T>
 __device__ __forceinline__ uint32_t block_scale(const Raw8<T> &r)

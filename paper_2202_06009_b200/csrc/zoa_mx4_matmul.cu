@@ -898,8 +898,16 @@ extern "C" zoa_status zoa_mx4_linear_forward(const void *x, int x_type, size_t l
     const char *me = "zoa_mx4_linear_forward";
     if (m && n && k && (!xt || !wt || !work)) return ops_fail(ZOA_ERR_ARG, "%s: a NULL pointer", me);
     void *wq = static_cast<unsigned char *>(work) + zoa_mx4_size(m, k);
-    zoa_status st = zoa_mx4_quantize(x, x_type, m, k, ldx, work, xt, stream);
-    if (st == ZOA_OK) st = zoa_mx4_quantize(w, w_type, n, k, ldw, wq, wt, stream);
+    zoa_status st = mx4_check_source(me, x, x_type, m, k, ldx, work, xt);
+    if (st == ZOA_OK) st = mx4_check_source(me, w, w_type, n, k, ldw, wq, wt);
+    if (st != ZOA_OK) return st;
+    if (x_type == w_type && m && n && k) {      // one launch for both
+        st = mx4_launch_both(me, x_type, mx4_both_job(x, x_type, m, k, ldx, work, xt), mx4_both_job(w, w_type, n, k, ldw, wq, wt),
+                             static_cast<cudaStream_t>(stream));
+    } else {
+        st = zoa_mx4_quantize(x, x_type, m, k, ldx, work, xt, stream);
+        if (st == ZOA_OK) st = zoa_mx4_quantize(w, w_type, n, k, ldw, wq, wt, stream);
+    }
     return st != ZOA_OK ? st : zoa_mx4_matmul(work, wq, m, n, k, y, x_type, ldy, stream);
 }
 

@@ -5,7 +5,7 @@ namespace zoa {
 namespace {
 
 constexpr int kRowWarps = 8;      // warps of a block of quantize_rows_kernel
-constexpr int kRowsPerWarp = 4;   // rows whose loads a warp has in flight at once
+constexpr int kRowsPerWarp = 4;   // rows a warp takes at once
 
 // The 4-byte scale words of a row's two groups of 128 columns, from the scale byte that every lane of block
 // lane / 4 holds: complete in lanes 0 and 16.
@@ -17,13 +17,15 @@ __device__ __forceinline__ uint32_t gather_scales(uint32_t byte, int lane)
     return w;
 }
 
-// One warp takes 256 columns (a line of a tile) of kRowsPerWarp rows at a time, a lane 8 neighbours: a block is four
-// lanes.  Warps walk over the matrix, the next rows' loads in flight beside this one's arithmetic.
+// A warp takes 256 columns (a line of a tile) of four rows at a time, a lane one block of 32 columns.  Warps walk over the
+// matrix, the next rows' loads in flight beside this one's arithmetic.  What bounds it beside memory is instructions:
+// a lane to a block needs no exchange for the block's maximum and one scale for 32 elements (with four lanes to a block
+// 16384 x 4096 took 35 us).
 template <typename T>
 __global__ void __launch_bounds__(kRowWarps * 32) quantize_rows_kernel(const T *__restrict__ x, long long rows, long long cols,
                                                                        long long ld, bool vec, uint8_t *__restrict__ out)
 {
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, row = lane >> 3, block = lane & 7;
     const int tiles_c = (int)mx_tiles(cols, kMxTileCols);
     // A warp's place (rows from r0, tile tile_c) moves on by the number of warps, kept as whole rows of tiles and a rest.
     const unsigned warps = gridDim.x * kRowWarps, me = blockIdx.x * kRowWarps + (threadIdx.x >> 5);
@@ -31,17 +33,57 @@ __global__ void __launch_bounds__(kRowWarps * 32) quantize_rows_kernel(const T *
     const int step_tiles = (int)(warps % tiles_c);
     long long next_r0 = (long long)(me / tiles_c) * kRowsPerWarp;
     int next_tile = (int)(me % tiles_c);
-    Raw8<T> next[kRowsPerWarp];
+    Raw32<T> next;
+    auto fetch = [&] {
+        const long long c = (long long)next_tile * kMxTileCols + block * kMxBlock, r = next_r0 + row;
+        if (r < rows) next = load32(x + r * ld + c, cols - c, vec);
+    };
+    fetch();
+    while (next_r0 < rows) {
+        const Raw32<T> v = next;
+        const long long r0 = next_r0;
+        const int tile_c = next_tile;
+        next_r0 += step_rows;
+        next_tile += step_tiles;
+        if (next_tile >= tiles_c) {
+            next_tile -= tiles_c;
+            next_r0 += kRowsPerWarp;
+        }
+        fetch();
+        uint32_t byte;
+        const uint4 codes = round32_block(v, byte);
+        const uint32_t scales = scale_word(byte, lane);
+        if (r0 + row >= rows) continue;
+        uint8_t *tile = out + ((r0 / kMxTileRows) * tiles_c + tile_c) * kMxTileBytes;       // kRowsPerWarp divides its rows
+        const int rr = (int)(r0 % kMxTileRows) + row;
+        *reinterpret_cast<uint4 *>(tile + mx_code_at(rr, block)) = codes;
+        if ((lane & 3) == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, block)) = scales;
+    }
+}
+
+// The same for binary32, where a lane's block would be a whole 128-byte line: four lanes to a block, so that a load takes
+// neighbours (8192 x 4096: 34 us, a lane to a block 43).
+__global__ void __launch_bounds__(kRowWarps * 32) quantize_rows_f32_kernel(const float *__restrict__ x, long long rows, long long cols, long long ld,
+                                                                          bool vec, uint8_t *__restrict__ out)
+{
+    const int lane = threadIdx.x & 31;
+    const int tiles_c = (int)mx_tiles(cols, kMxTileCols);
+    const unsigned warps = gridDim.x * kRowWarps, me = blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+    const long long step_rows = (long long)(warps / tiles_c) * kRowsPerWarp;
+    const int step_tiles = (int)(warps % tiles_c);
+    long long next_r0 = (long long)(me / tiles_c) * kRowsPerWarp;
+    int next_tile = (int)(me % tiles_c);
+    Raw8<float> next[kRowsPerWarp];
     auto fetch = [&] {
         const long long c = (long long)next_tile * kMxTileCols + lane * 8;
-        const T *at = x + next_r0 * ld + c;
+        const float *at = x + next_r0 * ld + c;
 #pragma unroll
         for (int i = 0; i < kRowsPerWarp; ++i, at += ld)
             if (next_r0 + i < rows) next[i] = load8(at, cols - c, vec);
     };
     fetch();
     while (next_r0 < rows) {
-        Raw8<T> v[kRowsPerWarp];
+        Raw8<float> v[kRowsPerWarp];
 #pragma unroll
         for (int i = 0; i < kRowsPerWarp; ++i) v[i] = next[i];
         const long long r0 = next_r0;
@@ -54,55 +96,61 @@ __global__ void __launch_bounds__(kRowWarps * 32) quantize_rows_kernel(const T *
         }
         fetch();
         const int there = (int)(rows - r0 < kRowsPerWarp ? rows - r0 : kRowsPerWarp), rr = (int)(r0 % kMxTileRows);
-        uint8_t *tile = out + ((r0 / kMxTileRows) * tiles_c + tile_c) * kMxTileBytes;       // kRowsPerWarp divides its rows
-        uint8_t *codes_at = tile + kMxScaleBytes + rr * 128 + (lane & 3) * 4, *scales_at = tile + mx_scale_at(rr, lane >> 2);
-        const int line = ((lane >> 2) ^ (rr & 7)) << 4;
+        uint8_t *tile = out + ((r0 / kMxTileRows) * tiles_c + tile_c) * kMxTileBytes;
 #pragma unroll
         for (int i = 0; i < kRowsPerWarp; ++i) {
             if (i >= there) break;
             const uint32_t byte = block_scale(v[i]);
             const uint32_t codes = byte == 255u ? 0u : codes8(v[i], mx_inverse(byte));
             const uint32_t scales = gather_scales(byte, lane);
-            *reinterpret_cast<uint32_t *>(codes_at + i * 128 + (line ^ (i << 4))) = codes;
-            if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(scales_at + i * 16) = scales;
+            *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr + i, lane >> 2) + (lane & 3) * 4) = codes;
+            if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr + i, lane >> 2)) = scales;
         }
     }
 }
 
 // One block takes 128 x 128 elements: rounds them along the rows as it loads them, keeps them in shared memory and
-// rounds them along the columns (the rows of the transposed matrix) from there, a thread 32 rows of one column (of a
-// pair of columns for the 16-bit types).  Four neighbouring lanes take the four blocks of a column, so that they write
-// 64 bytes of a line together; the columns' places in shared memory are shifted by 8 words for each block of rows, so
-// that those lanes read different banks.
+// rounds them along the columns (the rows of the transposed matrix) from there.  Along the rows a thread takes one block
+// of 32 columns at a time, along the columns 32 rows of one column (of a pair of columns for the 16-bit types).  Four
+// neighbouring lanes take the four blocks of a row or column, so that they write 64 bytes of a line together; the
+// columns' places in shared memory are shifted by 8 words for each block of rows, so that those lanes read different
+// banks.  (binary32: as in quantize_rows_f32_kernel along the rows.)
 constexpr int kBothThreads = 256;
 constexpr int kBothSide = 128;
 template <typename T>
-__global__ void __launch_bounds__(kBothThreads) quantize_both_kernel(const T *__restrict__ x, long long rows, long long cols,
-                                                                     long long ld, bool vec, uint8_t *__restrict__ out,
-                                                                     uint8_t *__restrict__ out_t)
+constexpr int kBothPitch = kBothSide * (int)sizeof(T) / 4 + 4;      // words a row
+template <typename T>
+__global__ void __launch_bounds__(kBothThreads, sizeof(T) == 4 ? 3 : 4) quantize_both_kernel(const BothJob first, const BothJob second, const unsigned first_blocks)
 {
-    constexpr int kRowWords = kBothSide * (int)sizeof(T) / 4, kPasses = kBothSide / 16;
+    constexpr int kRowWords = kBothSide * (int)sizeof(T) / 4, kPitch = kBothPitch<T>;
     extern __shared__ __align__(16) unsigned char both_smem[];
-    uint32_t *tile_s = reinterpret_cast<uint32_t *>(both_smem);   // [128][kRowWords]
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long c0 = (long long)blockIdx.x * kBothSide, r0 = (long long)blockIdx.y * kBothSide;
+    uint32_t *tile_s = reinterpret_cast<uint32_t *>(both_smem);   // [128][kPitch]
+    const bool is_second = blockIdx.x >= first_blocks;
+    const BothJob &job = is_second ? second : first;
+    const long long rows = job.rows, cols = job.cols, ld = job.ld;
+    const T *x = static_cast<const T *>(job.x);
+    const unsigned index = is_second ? blockIdx.x - first_blocks : blockIdx.x, across = (unsigned)mx_tiles(cols, kBothSide);
+    const long long c0 = (long long)(index % across) * kBothSide, r0 = (long long)(index / across) * kBothSide;
+    const int lane = threadIdx.x & 31, blk = lane & 3;
     const long long tiles_c = mx_tiles(cols, kMxTileCols), tiles_ct = mx_tiles(rows, kMxTileCols);
-    const int half = lane >> 4, l16 = lane & 15;
     const int group = (int)((c0 / kBothSide) & 1);                      // which half of a tile's columns
-    uint8_t *tile = out ? out + ((r0 / kMxTileRows) * tiles_c + c0 / kMxTileCols) * kMxTileBytes : nullptr;
+    uint8_t *tile = job.out ? job.out + ((r0 / kMxTileRows) * tiles_c + c0 / kMxTileCols) * kMxTileBytes : nullptr;
     const bool last_half = group == 0 && c0 + kBothSide >= cols;        // the tile's second half has no block of its own
-
-    // A half warp holds 128 columns of a row; all loads first.  Rows that are not aligned go element by element to
-    // shared memory, where they are.
-    Raw8<T> v[kPasses];
-    auto word_at = [&](int rr, int k) { return tile_s + rr * kRowWords + ((l16 * Raw8<T>::kWords + k) ^ ((rr >> 5) * 8)); };
-    if (vec) {
-#pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-            const int rr = i * 16 + warp * 2 + half;
-            v[i] = load8(x + (r0 + rr) * ld + c0 + l16 * 8, r0 + rr < rows ? cols - c0 - l16 * 8 : 0, true);
+    auto word_at = [&](int rr, int word) { return tile_s + rr * kPitch + (word ^ ((rr >> 5) * 8)); };
+    // One row's (column's) codes and scale, to line r of `to`; the four lanes' scale bytes make a word.
+    auto store_line = [&](uint8_t *to, int r, int half, bool exists, bool clear_next, uint32_t byte, const uint4 &codes) {
+        const uint32_t scales = scale_word(byte, lane);
+        if (!exists) return;
+        *reinterpret_cast<uint4 *>(to + mx_code_at(r, half * 4 + blk)) = codes;
+        if (blk == 0) *reinterpret_cast<uint32_t *>(to + mx_scale_at(r, half * 4)) = scales;
+        if (clear_next) {
+            *reinterpret_cast<uint4 *>(to + mx_code_at(r, 4 + blk)) = make_uint4(0, 0, 0, 0);
+            if (blk == 0) *reinterpret_cast<uint32_t *>(to + mx_scale_at(r, 4)) = 0u;
         }
-    } else {
+    };
+
+    // Along the rows; all loads first.  Rows that are not aligned go element by element to shared memory, where they are.
+    if (!job.vec) {
         using Bits = typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type;
         const int col = threadIdx.x % kBothSide;
 #pragma unroll 8
@@ -110,69 +158,78 @@ __global__ void __launch_bounds__(kBothThreads) quantize_both_kernel(const T *__
             const int rr = i * 2 + threadIdx.x / kBothSide;
             Bits e = 0;
             if (r0 + rr < rows && c0 + col < cols) e = reinterpret_cast<const Bits *>(x)[(r0 + rr) * ld + c0 + col];
-            const int word = sizeof(T) == 4 ? col : col >> 1;
-            Bits *at = reinterpret_cast<Bits *>(tile_s + rr * kRowWords + (word ^ ((rr >> 5) * 8)));
-            at[sizeof(T) == 4 ? 0 : col & 1] = e;
+            reinterpret_cast<Bits *>(word_at(rr, sizeof(T) == 4 ? col : col >> 1))[sizeof(T) == 4 ? 0 : col & 1] = e;
         }
         __syncthreads();
+    }
+    // Between registers and shared memory, whichever has them.
+    auto settle = [&](uint32_t *w, int words, int rr, int first) {
+#pragma unroll
+        for (int k = 0; k < words; k += 4) {
+            uint4 *at = reinterpret_cast<uint4 *>(word_at(rr, first + k));
+            if (job.vec) {
+                *at = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+            } else {
+                const uint4 v = *at;
+                w[k] = v.x;
+                w[k + 1] = v.y;
+                w[k + 2] = v.z;
+                w[k + 3] = v.w;
+            }
+        }
+    };
+    if constexpr (sizeof(T) == 4) {      // four lanes to a block, half a warp to a row, as in quantize_rows_f32_kernel
+        constexpr int kPasses = kBothSide / 16;
+        const int half = lane >> 4, l16 = lane & 15, warp = threadIdx.x >> 5;
+        Raw8<T> v[kPasses];
 #pragma unroll
         for (int i = 0; i < kPasses; ++i) {
             const int rr = i * 16 + warp * 2 + half;
+            if (job.vec) v[i] = load8(x + (r0 + rr) * ld + c0 + l16 * 8, r0 + rr < rows ? cols - c0 - l16 * 8 : 0, true);
+        }
 #pragma unroll
-            for (int k = 0; k < Raw8<T>::kWords; k += 4) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(word_at(rr, k));
-                v[i].w[k] = w.x;
-                v[i].w[k + 1] = w.y;
-                v[i].w[k + 2] = w.z;
-                v[i].w[k + 3] = w.w;
+        for (int i = 0; i < kPasses; ++i) {
+            const int rr = i * 16 + warp * 2 + half;
+            settle(v[i].w, 8, rr, l16 * 8);
+            if (!tile) continue;
+            const uint32_t byte = block_scale(v[i]), codes = byte == 255u ? 0u : codes8(v[i], mx_inverse(byte));
+            const uint32_t scales = gather_scales(byte, lane);
+            if (r0 + rr >= rows) continue;
+            *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr, group * 4 + (l16 >> 2)) + (l16 & 3) * 4) = codes;
+            if (l16 == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, group * 4)) = scales;
+            if (last_half) {
+                *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr, 4 + (l16 >> 2)) + (l16 & 3) * 4) = 0u;
+                if (l16 == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, 4)) = 0u;
             }
         }
-    }
+    } else {
+        Raw32<T> v[2];
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-        const int rr = i * 16 + warp * 2 + half;
-        if (vec) {
-#pragma unroll
-            for (int k = 0; k < Raw8<T>::kWords; k += 4)
-                *reinterpret_cast<uint4 *>(word_at(rr, k)) = make_uint4(v[i].w[k], v[i].w[k + 1], v[i].w[k + 2], v[i].w[k + 3]);
+        for (int i = 0; i < 2; ++i) {
+            const int rr = i * 64 + (threadIdx.x >> 2);
+            const long long c = c0 + blk * kMxBlock;
+            if (job.vec) v[i] = load32(x + (r0 + rr) * ld + c, r0 + rr < rows ? cols - c : 0, true);
         }
-        if (!tile) continue;
-        const uint32_t byte = block_scale(v[i]);
-        const uint32_t codes = byte == 255u ? 0u : codes8(v[i], mx_inverse(byte));
-        const uint32_t scales = gather_scales(byte, lane);
-        if (r0 + rr >= rows) continue;
-        *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr, group * 4 + (l16 >> 2)) + (l16 & 3) * 4) = codes;
-        if (l16 == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, group * 4)) = scales;
-        if (last_half) {
-            *reinterpret_cast<uint32_t *>(tile + mx_code_at(rr, 4 + (l16 >> 2)) + (l16 & 3) * 4) = 0u;
-            if (l16 == 0) *reinterpret_cast<uint32_t *>(tile + mx_scale_at(rr, 4)) = 0u;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int rr = i * 64 + (threadIdx.x >> 2);
+            settle(v[i].w, Raw32<T>::kWords, rr, blk * Raw32<T>::kWords);
+            if (!tile) continue;
+            uint32_t byte;
+            const uint4 codes = round32_block(v[i], byte);
+            store_line(tile, rr, group, r0 + rr < rows, last_half, byte, codes);
         }
     }
     __syncthreads();
     const int group_t = (int)((r0 / kBothSide) & 1);
     const bool last_half_t = group_t == 0 && r0 + kBothSide >= rows;
-    uint8_t *tile_t = out_t + ((c0 / kMxTileRows) * tiles_ct + r0 / kMxTileCols) * kMxTileBytes;
-    const int blk = lane & 3;
-    // One column's codes and scale; the four lanes' scale bytes make a word.
-    auto store_column = [&](int cc, uint32_t byte, uint4 codes) {
-        uint32_t word = byte << (8 * blk);
-        word |= __shfl_xor_sync(0xffffffffu, word, 1);
-        word |= __shfl_xor_sync(0xffffffffu, word, 2);
-        if (c0 + cc >= cols) return;
-        if (byte == 255u) codes = make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4 *>(tile_t + mx_code_at(cc, group_t * 4 + blk)) = codes;
-        if (blk == 0) *reinterpret_cast<uint32_t *>(tile_t + mx_scale_at(cc, group_t * 4)) = word;
-        if (last_half_t) {
-            *reinterpret_cast<uint4 *>(tile_t + mx_code_at(cc, 4 + blk)) = make_uint4(0, 0, 0, 0);
-            if (blk == 0) *reinterpret_cast<uint32_t *>(tile_t + mx_scale_at(cc, 4)) = 0u;
-        }
-    };
+    uint8_t *tile_t = job.out_t + ((c0 / kMxTileRows) * tiles_ct + r0 / kMxTileCols) * kMxTileBytes;
     for (int col = threadIdx.x >> 2; col < kRowWords; col += kBothThreads / 4) {     // a word: one column, or a pair
         uint32_t w[32];
         uint32_t m = 0;
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
-            w[k] = tile_s[(blk * 32 + k) * kRowWords + (col ^ (blk * 8))];
+            w[k] = *word_at(blk * 32 + k, col);
             m = larger<T>(m, w[k]);
         }
         constexpr int kColumns = 4 / (int)sizeof(T);
@@ -201,10 +258,13 @@ __global__ void __launch_bounds__(kBothThreads) quantize_both_kernel(const T *__
                 }
             }
 #pragma unroll
-            for (int h = 0; h < kColumns; ++h) codes[h][q] = mx_codes8(p[h]);
+            for (int h = 0; h < kColumns; ++h) codes[h][q] = byte[h] == 255u ? 0u : mx_codes8(p[h]);
         }
 #pragma unroll
-        for (int h = 0; h < kColumns; ++h) store_column(kColumns * col + h, byte[h], make_uint4(codes[h][0], codes[h][1], codes[h][2], codes[h][3]));
+        for (int h = 0; h < kColumns; ++h) {
+            const int cc = kColumns * col + h;
+            store_line(tile_t, cc, group_t, c0 + cc < cols, last_half_t, byte[h], make_uint4(codes[h][0], codes[h][1], codes[h][2], codes[h][3]));
+        }
     }
 }
 
@@ -290,6 +350,40 @@ __global__ void __launch_bounds__(kRowWarps * 32) dequantize_kernel(const uint8_
 bool rows_vectorised(const void *p, int dtype, size_t ld) { return aligned16(p) && ld * dtype_bytes(dtype) % 16 == 0; }
 
 }  // namespace
+
+zoa_status mx4_check_source(const char *me, const void *x, int dtype, size_t rows, size_t cols, size_t ld, const void *out, const void *out_t)
+{
+    if (!dtype_ok(dtype)) return ops_fail(ZOA_ERR_ARG, "%s: unknown element type %d", me, dtype);
+    if (rows > kMxMaxSide || cols > kMxMaxSide) return ops_fail(ZOA_ERR_ARG, "%s: rows and cols must be at most 2^30", me);
+    if (rows == 0 || cols == 0) return ZOA_OK;
+    if (!x || (!out && !out_t)) return ops_fail(ZOA_ERR_ARG, "%s: a NULL pointer", me);
+    if (ld < cols) return ops_fail(ZOA_ERR_ARG, "%s: ld must be at least cols", me);
+    if (reinterpret_cast<uintptr_t>(x) % dtype_bytes(dtype)) return ops_fail(ZOA_ERR_ARG, "%s: x is not aligned to its element type", me);
+    if (!aligned16(out) || !aligned16(out_t)) return ops_fail(ZOA_ERR_ARG, "%s: out and out_t must be 16-byte aligned", me);
+    if (out_t && mx_tiles((long long)rows, kBothSide) * mx_tiles((long long)cols, kBothSide) > (1ll << 30))
+        return ops_fail(ZOA_ERR_ARG, "%s: at most 2^44 elements when out_t is asked for", me);
+    return ZOA_OK;
+}
+
+BothJob mx4_both_job(const void *x, int dtype, size_t rows, size_t cols, size_t ld, void *out, void *out_t)
+{
+    return BothJob{x, static_cast<uint8_t *>(out), static_cast<uint8_t *>(out_t), (long long)rows, (long long)cols, (long long)ld,
+                   (int)rows_vectorised(x, dtype, ld)};
+}
+
+zoa_status mx4_launch_both(const char *me, int dtype, const BothJob &a, const BothJob &b, cudaStream_t s)
+{
+    const long long of_a = mx_tiles(a.rows, kBothSide) * mx_tiles(a.cols, kBothSide), of_b = mx_tiles(b.rows, kBothSide) * mx_tiles(b.cols, kBothSide);
+    with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        constexpr int kSmem = kBothSide * kBothPitch<T> * 4;
+        static SmemLimit limit;
+        if (limit.ensure(quantize_both_kernel<T>, kSmem) != cudaSuccess) return;   // the launch below reports it
+        quantize_both_kernel<T><<<(unsigned)(of_a + of_b), kBothThreads, kSmem, s>>>(a, b, (unsigned)of_a);
+    });
+    return ops_launched(me);
+}
+
 }  // namespace zoa
 
 using namespace zoa;
@@ -304,35 +398,19 @@ extern "C" zoa_status zoa_mx4_quantize(const void *x, int dtype, size_t rows, si
                                        void *stream)
 {
     const char *me = "zoa_mx4_quantize";
-    if (!dtype_ok(dtype)) return ops_fail(ZOA_ERR_ARG, "%s: unknown element type %d", me, dtype);
-    if (rows > kMxMaxSide || cols > kMxMaxSide) return ops_fail(ZOA_ERR_ARG, "%s: rows and cols must be at most 2^30", me);
-    if (rows == 0 || cols == 0) return ZOA_OK;
-    if (!x || (!out && !out_t)) return ops_fail(ZOA_ERR_ARG, "%s: a NULL pointer", me);
-    if (ld < cols) return ops_fail(ZOA_ERR_ARG, "%s: ld must be at least cols", me);
-    if (reinterpret_cast<uintptr_t>(x) % dtype_bytes(dtype)) return ops_fail(ZOA_ERR_ARG, "%s: x is not aligned to its element type", me);
-    if (!aligned16(out) || !aligned16(out_t)) return ops_fail(ZOA_ERR_ARG, "%s: out and out_t must be 16-byte aligned", me);
-    const bool vec = rows_vectorised(x, dtype, ld);
+    const zoa_status st = mx4_check_source(me, x, dtype, rows, cols, ld, out, out_t);
+    if (st != ZOA_OK || rows == 0 || cols == 0) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const long long R = (long long)rows, C = (long long)cols, L = (long long)ld;
-    if (!out_t) {
-        const long long blocks = mx_tiles(mx_tiles(R, kRowsPerWarp) * mx_tiles(C, kMxTileCols), kRowWarps), most = 4ll * ops_sm_count();
-        with_type(dtype, [&](auto t) {
-            using T = decltype(t);
-            quantize_rows_kernel<T><<<(unsigned)(blocks < most ? blocks : most), kRowWarps * 32, 0, s>>>(static_cast<const T *>(x), R, C, L, vec,
-                                                                                                       static_cast<uint8_t *>(out));
-        });
-        return ops_launched(me);
-    }
-    if (mx_tiles(R, kBothSide) > 65535) return ops_fail(ZOA_ERR_ARG, "%s: at most 8388480 rows when out_t is asked for", me);
+    if (out_t) return mx4_launch_both(me, dtype, mx4_both_job(x, dtype, rows, cols, ld, out, out_t), BothJob{}, s);
+    const bool vec = rows_vectorised(x, dtype, ld);
+    const long long R = (long long)rows, C = (long long)cols;
+    const long long blocks = mx_tiles(mx_tiles(R, kRowsPerWarp) * mx_tiles(C, kMxTileCols), kRowWarps), most = 4ll * ops_sm_count();
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        const int smem = kBothSide * kBothSide * (int)sizeof(T);
-        if (smem > 48 * 1024) {
-            static SmemLimit limit;
-            if (limit.ensure(quantize_both_kernel<T>, smem) != cudaSuccess) return;   // the launch below reports it
-        }
-        quantize_both_kernel<T><<<dim3((unsigned)mx_tiles(C, kBothSide), (unsigned)mx_tiles(R, kBothSide)), kBothThreads, smem, s>>>(
-            static_cast<const T *>(x), R, C, L, vec, static_cast<uint8_t *>(out), static_cast<uint8_t *>(out_t));
+        const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+        uint8_t *to = static_cast<uint8_t *>(out);
+        if constexpr (sizeof(T) == 4) quantize_rows_f32_kernel<<<grid, kRowWarps * 32, 0, s>>>(static_cast<const T *>(x), R, C, (long long)ld, vec, to);
+        else quantize_rows_kernel<T><<<grid, kRowWarps * 32, 0, s>>>(static_cast<const T *>(x), R, C, (long long)ld, vec, to);
     });
     return ops_launched(me);
 }

@@ -149,7 +149,7 @@ def mx4_linear(x, w, out=None):
     if w.data.device != device:
         raise ValueError("x and w must be on the same device")
     if out is None:
-        out, ld = torch.empty((m, n), dtype=x.dtype, device=device), n
+        out, ld = x.new_empty((m, n)), n
     else:
         ld = _check_result(out, m, n, x.dtype, device)
     size = _lib.zoa_mx4_linear_work(m, n, k)
@@ -177,7 +177,7 @@ def mx4_linear_forward(x, w):
         raise ValueError(f"x is {tuple(x.shape)}, w is {tuple(w.shape)}: their columns must agree")
     if w.device != device:
         raise ValueError("x and w must be on the same device")
-    y = torch.empty((m, n), dtype=x.dtype, device=device)
+    y = x.new_empty((m, n))
     xt = _size(k, m)
     saved = _bytes(xt + _size(k, n), device)
     work = _bytes(_size(m, k) + _size(n, k), device)
