@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) quantize_rows_f32_kernel(const
 constexpr int kBothThreads = 256;
 constexpr int kBothSide = 128;
 template <typename T>
-constexpr int kBothPitch = kBothSide * (int)sizeof(T) / 4 + 4;      // words a row
+constexpr int kBothPitch = kBothSide * (int)sizeof(T) / 4 + (sizeof(T) == 4 ? 0 : 4);      // words a row
 template <typename T>
 __global__ void __launch_bounds__(kBothThreads, sizeof(T) == 4 ? 3 : 4) quantize_both_kernel(const BothJob first, const BothJob second, const unsigned first_blocks)
 {
@@ -303,7 +303,8 @@ __global__ void __launch_bounds__(kRowWarps * 32) dequantize_kernel(const uint8_
     const long long tile_c = blockIdx.x, tiles_c = gridDim.x;
     const long long c = tile_c * kMxTileCols + lane * 8;
     const long long r0 = ((long long)blockIdx.y * kRowWarps + warp) * kReadRows;
-    if (c >= cols || r0 >= rows) return;
+    __shared__ __align__(16) float turn[kRowWarps][kMxTileCols];       // a row, for stores of neighbours where rows are not aligned
+    if (r0 >= rows || (vec && c >= cols)) return;
     const int there = (int)(rows - r0 < kReadRows ? rows - r0 : kReadRows), rr = (int)(r0 % kMxTileRows);       // kReadRows divides a tile's rows
     const uint8_t *tile = in + ((r0 / kMxTileRows) * tiles_c + tile_c) * kMxTileBytes;
     const uint8_t *codes_at = tile + kMxScaleBytes + rr * 128 + (lane & 3) * 4, *scales_at = tile + mx_scale_at(rr, lane >> 2);
@@ -339,10 +340,18 @@ __global__ void __launch_bounds__(kRowWarps * 32) dequantize_kernel(const uint8_
         if (whole) {
             *reinterpret_cast<uint4 *>(dst) = Vec<T>::pack(v);
             if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4 *>(dst + 4) = Vec<T>::pack(v + 4);
-        } else {
+        } else if (vec) {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (c + k < cols) dst[k] = from_f32<T>(v[k]);
+        } else {
+            *reinterpret_cast<float4 *>(&turn[warp][lane * 8]) = make_float4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<float4 *>(&turn[warp][lane * 8 + 4]) = make_float4(v[4], v[5], v[6], v[7]);
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c - lane * 8 + k * 32 + lane < cols) dst[k * 32 - lane * 7] = from_f32<T>(turn[warp][k * 32 + lane]);
+            __syncwarp();
         }
     }
 }
