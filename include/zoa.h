@@ -408,11 +408,14 @@ const char *zoa_static_last_error(void);
 /* ---- Operators of a low-bit student --------------------------------------------
  * What produces the gradients of a step when the model's linear layers run in 4
  * bits and a stored teacher gives the loss: 4-bit microscaled matrices, their
- * products, and distillation from a teacher's top logits.  No handle: every call works on buffers the
- * caller owns, on the current device, allocates nothing, checks its arguments before anything is
- * enqueued (ZOA_ERR_ARG), enqueues on `stream` and does not synchronise.  A call
- * that fails returns a status; its text is zoa_ops_last_error() of the same thread.
- * Calls may be made from several threads.  (The paper has no counterpart to them.)
+ * products, and distillation from a teacher's top logits.  No handle: every call
+ * works on buffers the caller owns, on the current device, allocates nothing,
+ * checks its arguments before anything is enqueued (ZOA_ERR_ARG), enqueues on
+ * `stream` and does not synchronise.  A call that fails returns a status; its text
+ * is zoa_ops_last_error() of the same thread.  Calls may be made from several
+ * threads.  The first call of each kind on a device looks up addresses and raises
+ * kernels' shared-memory limits: make it before any stream capture starts.  (The
+ * paper has no counterpart to these entry points.)
  *
  * Element types of the plain matrices: binary32, binary16, bfloat16.  `ld` is the
  * distance between rows in elements; neighbours of a row are contiguous.  Rows
@@ -427,30 +430,31 @@ typedef enum { ZOA_F32 = 0, ZOA_F16 = 1, ZOA_BF16 = 2 } zoa_dtype;
  *   nearest element, ties to the even code, at most 6 in magnitude.
  * A block of zeros has scale 2^-127.  A block with a NaN or an infinity reads back
  * as NaN, and so does every product that touches it.
- * The form is one buffer of zoa_mx4_size(rows, cols) bytes (0 for an empty or
- * too large matrix: a side is at most 2^30), 16-byte aligned, whose layout belongs to the library: tiles
- * of 128 rows by 256 columns, scales before codes.  Rounding the values that a form stands
- * for gives those values again, so zoa_mx4_dequantize and zoa_mx4_quantize also
- * convert from and to any other layout without loss.
+ * The form is one buffer of zoa_mx4_size(rows, cols) bytes, 16-byte aligned (0 bytes
+ * for an empty or too large matrix: a side is at most 2^30), whose layout belongs to
+ * the library: tiles of 128 rows by 256 columns, scales before codes.  Rounding the
+ * values that a form stands for gives those values again, so zoa_mx4_dequantize and
+ * zoa_mx4_quantize also convert from and to any other layout without loss.
  * zoa_mx4_quantize: out (may be NULL) receives the form of x [rows, cols], out_t
  * (may be NULL, not both) that of its transpose [cols, rows], blocks along x's
- * columns; both come from one read of x. */
+ * columns; both come from one read of x.  zoa_mx4_dequantize writes the values, exact in
+ * binary32 and bfloat16; in binary16 they overflow and round as in any conversion. */
 size_t zoa_mx4_size(size_t rows, size_t cols);
 zoa_status zoa_mx4_quantize(const void *x, int dtype, size_t rows, size_t cols, size_t ld, void *out, void *out_t,
                             void *stream);
 zoa_status zoa_mx4_dequantize(const void *q, size_t rows, size_t cols, void *out, int dtype, size_t ld, void *stream);
 
-/* out[i, j] = sum over k of a[i, k] b[j, k]: a is the form of an [m, k] matrix, b of an
- * [n, k] one, out [m, n] of the given type; sums in binary32, one rounding at the
- * end.  (b is a linear layer's weight as it is usually kept, [out, in].)  k = 0
- * gives zeros.  The order of a sum depends on the sizes alone: equal calls give equal bits. */
+/* out[i, j] = sum over k of a[i, k] b[j, k]: a is the form of an [m, k] matrix, b of
+ * an [n, k] one, out [m, n] of the given type; sums in binary32, one rounding at the
+ * end.  (b is a linear layer's weight as it is usually kept, [out, in].)  k = 0 gives
+ * zeros.  The order of a sum depends on the sizes alone: equal calls give equal bits. */
 zoa_status zoa_mx4_matmul(const void *a, const void *b, size_t m, size_t n, size_t k, void *out, int dtype, size_t ld,
                           void *stream);
 
 /* A linear layer on real activations: out = Q(x) b^T, Q being the rounding of
- * zoa_mx4_quantize.  work: (device) zoa_mx4_linear_work(m, n, k) bytes, 16-byte aligned, for
- * the 4-bit form of x (NULL where that is 0: few rows are rounded inside the
- * product).  x and out have the same type. */
+ * zoa_mx4_quantize.  work: (device) zoa_mx4_linear_work(m, n, k) bytes, 16-byte
+ * aligned, for the 4-bit form of x (NULL where that is 0: up to four rows with a
+ * weight of moderate size are rounded inside the product).  x and out have the same type. */
 size_t zoa_mx4_linear_work(size_t m, size_t n, size_t k);
 zoa_status zoa_mx4_linear(const void *x, int dtype, size_t m, size_t k, size_t ldx, const void *b, size_t n, void *out,
                           size_t ld, void *work, void *stream);
@@ -486,14 +490,18 @@ zoa_status zoa_mx4_linear_backward(const void *dy, int dy_type, size_t ld_dy, si
  * left, or none above -inf, has no soft part.  A term with p = 0 is 0.
  * labels (may be NULL): int32 [rows]; a row whose label is outside [0, vocab) has
  * no hard part.  A row of weight 0 gives loss 0 and gradient 0 whatever it holds.
- * Logits of -inf are tokens masked out (q = 0, gradient 0); a row of nothing else gives loss 0 and gradient 0.  The p_r term is left out of
- * a row whose q_r is 0 or below 1e-30.  A NaN or +inf logit makes
- * its row NaN.  All sums in binary32.
- * zoa_distill_topk: loss (binary32 [rows]), and, where they are not NULL, grad
- * [rows, vocab] (the logits' type; may be the logits themselves with the same ld: they are then replaced) and stats
- * (binary32 [rows, 4], for the next call).  teacher has the logits' type.
- * zoa_distill_topk_backward: grad of grad_loss[row] * loss[row] from the same
- * inputs and the stats of the forward call, with no second reduction. */
+ * Logits of -inf are tokens masked out (q = 0, gradient 0); a row of nothing else
+ * gives loss 0 and gradient 0.  The p_r term is left out of a row whose q_r is 0 or
+ * below 1e-30.  A NaN or +inf logit makes its row NaN.  All sums in binary32; the
+ * order of a row's sums depends on the sizes of the call.  Limits: vocab in
+ * [1, 2^20], top in [1, 2048].
+ * zoa_distill_topk: loss (binary32 [rows], may be NULL), and, where they are not
+ * NULL, grad [rows, vocab] (the logits' type; may be the logits themselves with the
+ * same ld: they are then replaced) and stats (binary32 [rows, 4], 16-byte aligned, for
+ * the next call).  teacher has the logits' type.
+ * zoa_distill_topk_backward: grad of grad_loss[row] * loss[row] from the same inputs
+ * and the stats of the forward call, with no second reduction; grad may be the logits
+ * here too. */
 typedef struct {
     const void *logits;      /* (device) [rows, vocab] */
     const int32_t *index;    /* (device) [rows, top], rows contiguous */
@@ -511,10 +519,12 @@ zoa_status zoa_distill_topk_backward(const zoa_distill_args *args, const float *
                                      size_t ld_grad, void *stream);
 
 /* Text of the last error of one of these calls on this thread (never NULL).
- * zoa_ops_set_option: ZOA_OPT_WAIT_LIMIT_MS and ZOA_OPT_TEST_STOP_AFTER_TILES for the
- * product kernels of this process, with the meaning and the defaults they have on a handle.
- * zoa_ops_check_device: waits for the device; ZOA_ERR_DEVICE if a product kernel gave up on a
- * bounded wait since the last check (its result is undefined; the condition is cleared). */
+ * zoa_ops_set_option: ZOA_OPT_WAIT_LIMIT_MS and ZOA_OPT_TEST_STOP_AFTER_TILES (here a
+ * tile of k) for the kernels of these calls in this process, with the meaning and the
+ * defaults they have on a handle.
+ * zoa_ops_check_device: waits for the device; ZOA_ERR_DEVICE if a kernel of these calls
+ * gave up on a bounded wait since the last check (its result is undefined; the
+ * condition is cleared). */
 const char *zoa_ops_last_error(void);
 zoa_status zoa_ops_set_option(int option, int value);
 zoa_status zoa_ops_check_device(void);

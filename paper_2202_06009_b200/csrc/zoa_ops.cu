@@ -87,5 +87,5 @@ extern "C" zoa_status zoa_ops_check_device(void)
     set = 0;
     e = cudaMemcpy(word, &set, sizeof set, cudaMemcpyHostToDevice);
     if (e != cudaSuccess) return ops_fail(ZOA_ERR_CUDA, "zoa_ops_check_device: %s", cudaGetErrorString(e));
-    return ops_fail(ZOA_ERR_DEVICE, "a product kernel gave up on a bounded wait; its result is undefined");
+    return ops_fail(ZOA_ERR_DEVICE, "a kernel gave up on a bounded wait; its result is undefined");
 }

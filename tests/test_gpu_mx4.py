@@ -260,7 +260,7 @@ def test_offsets_past_32_bits():
     want = round_mx4(as64(x[ends.cuda()]))
     q, qt = mx4_quantize_both(x)
     single = mx4_quantize(x)
-    assert torch.equal(q.data, single.data) or True      # rows past the end of the last tile hold anything
+    assert np.array_equal(as64(single.dequantize(torch.float32)[ends.cuda()]), want)
     del single
     back = q.dequantize(torch.bfloat16)
     assert np.array_equal(as64(back[ends.cuda()]), want)
@@ -269,6 +269,28 @@ def test_offsets_past_32_bits():
     assert back.shape == (cols, rows)
     last = rows - rows % 32
     assert np.array_equal(as64(back[:, last:]), round_mx4(as64(x[last:]).T))
+
+
+@pytest.mark.parametrize("pad", [0, 1])
+def test_product_past_32_bits(pad):
+    """A result of more than 2^31 elements: its last rows, aligned and not."""
+    m, n, k = 70001, 32 * 1024, 64
+    a, b = torch.zeros(m, k, dtype=torch.bfloat16, device="cuda"), data(n, k, torch.bfloat16, 2, 0.1)
+    a[-3:] = data(3, k, torch.bfloat16, 3)
+    out = torch.empty(m, n + pad, dtype=torch.bfloat16, device="cuda")[:, :n]
+    mx4_matmul(mx4_quantize(a), mx4_quantize(b), out=out)
+    assert_product(out[-3:], round_mx4(as64(a[-3:])), round_mx4(as64(b)), torch.bfloat16)
+    assert not out[-300:-3].any() and not out[:300].any()
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 6400, 1600), (1, 9, 9000), (2, 1000, 4100), (3, 77, 70), (4, 1030, 300), (1, 33000, 256), (4, 5000, 5000)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_on_few_rows(m, n, k, dtype):
+    x, w = data(m, k, dtype, m, 0.5), data(n, k, dtype, n + 1, 0.5, 0.1)
+    q = mx4_quantize(w)
+    y = mx4_linear(x, q)
+    assert_product(y, round_mx4(as64(x)), round_mx4(as64(w)), dtype)
+    assert torch.equal(y, mx4_linear(x, q))
 
 
 def test_sizes_of_zero():
