@@ -109,7 +109,7 @@ struct MatmulArgs {
     long long m, n, ld;
     int tiles_k;              // tiles of 256 columns
     int k_steps;              // steps of 64 columns, the last one perhaps partly zeros
-    int vec;                  // rows of `out` are 16-byte (1) or 32-byte (2) aligned
+    bool vec;                 // rows of `out` are 16-byte aligned
     int test_stop;            // > 0: the copies stop at this k tile (error-path test)
     WaitLimit limit;
 };
@@ -299,17 +299,23 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g, const i
 
 // ---- pairs of SMs, large products --------------------------------------------------------------------------
 // A cluster of two blocks computes 256 x 256 of C at a time, each block the sums of 128 rows, and walks over the tiles
-// with a stride: 16384 x 8192 x 4096 in 213 us (5.2 PFLOP/s; 254 us back to back under the power limit, 4.3),
-// 8192 x 8192 x 16384 in 385 (5.7).  A product of 256 x 256 x 64 takes 203 cycles of the pair's tensor cores whatever else
-// runs, which is what bounds it; between tiles they wait about 1.5 us for the sums to be taken.  Every byte of A goes to one SM and every byte of B's codes too (the tensor cores read the partner's
-// half from its shared memory); only B's scales go to both.  The sums fill half of tensor memory; the scales of the
-// stages in flight take the rest, so the next tile starts when the sums have been taken to registers, not when they
-// have been stored.
+// with a stride: 16384 x 8192 x 4096 in 208 us (5.3 PFLOP/s; about 250 us back to back under the power limit),
+// 8192 x 8192 x 16384 in 377 (5.8).  What bounds it is the copies that feed it: a product of 256 x 256 x 64 takes 203
+// cycles with the copies of the next ones beside it, 43 bytes a cycle into every SM, and 169 on operands that are there
+// already; results that leave in the same time add to that (short sums: 16384 x 6400 x 1600 81 us, nothing stored 68).
+// Every byte of A goes to one SM and every byte of B's codes too (the tensor cores read the partner's half from its
+// shared memory); only B's scales go to both.
 constexpr int kPairStages = 5;
 constexpr int kPairStageBytes = kMxTileBytes + 2 * kMxScaleBytes + kMxCodeBytes;    // A tile; B scales of both halves; B codes
 constexpr int kPairScaleColumns = 24;                                              // 8 for A, 16 for B
 constexpr int kPairThreads = 448;
-struct PairShared {
+// Where the sums of a pair's even and odd tiles lie: 256 columns from 0 and from 128.  They share 128 columns (the sums of
+// two tiles and the scales do not fit side by side); the next tile begins when these have been taken, which also says
+// that all of the tile before has been.
+constexpr int kPairOverlap = 128;
+static_assert(256 + kPairOverlap + kPairStages * kPairScaleColumns <= 512, "tensor memory has 512 columns");
+__device__ __forceinline__ uint32_t pair_sums_at(uint32_t round) { return round & 1 ? kPairOverlap : 0; }
+struct alignas(16) PairShared {
     unsigned long long full[kPairStages], scaled[kPairStages], empty[kPairStages], sums_full, sums_empty, finished;
     uint32_t tmem;
     int gave_up;
@@ -336,24 +342,38 @@ __device__ __forceinline__ PairTile pair_tile(const MatmulArgs &g, long long t, 
     return p;
 }
 
-// 32 neighbours of a row of the result, already of type T, where rows are aligned and hold all of them.
+// 128 bytes of each of a warp's 32 rows (lane = row, already of type T), turned through shared memory so that a store writes
+// whole lines; rows are 16-byte aligned.  With a lane storing 32-byte pieces of its own row the stores held the copies up:
+// 16384 x 6400 x 1600 to bfloat16 88 us, this way 84, and 81 where results leave the L2 before operands do; to binary32 123,
+// 108 and 103.
 template <typename T>
-__device__ __forceinline__ void store_row32(T *at, int vec, const uint32_t *w)
+__device__ __forceinline__ void store_lines(T *first, long long ld, int rows, int cols, const uint32_t *w, float *turn)
 {
-    constexpr int kWords = 32 * (int)sizeof(T) / 4;
-    uint32_t *dst = reinterpret_cast<uint32_t *>(at);
-    if (vec == 2) {
+    constexpr int kPiece = 16 / (int)sizeof(T);
+    const int lane = threadIdx.x & 31;
+    uint4 *pieces = reinterpret_cast<uint4 *>(turn);
+    __syncwarp();
 #pragma unroll
-        for (int k = 0; k < kWords; k += 8)
-            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + k), "r"(w[k]), "r"(w[k + 1]), "r"(w[k + 2]),
-                         "r"(w[k + 3]), "r"(w[k + 4]), "r"(w[k + 5]), "r"(w[k + 6]), "r"(w[k + 7])
-                         : "memory");
-    } else {
+    for (int p = 0; p < 8; ++p) pieces[lane * 8 + (p ^ (lane & 7))] = make_uint4(w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
+    __syncwarp();
+    const int col = (lane & 7) * kPiece;
+    T *at = first + (lane >> 3) * ld + col;
 #pragma unroll
-        for (int k = 0; k < kWords; k += 4) *reinterpret_cast<uint4 *>(dst + k) = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+    for (int i = 0; i < 8; ++i, at += 4 * ld) {
+        const int row = i * 4 + (lane >> 3);
+        if (row >= rows) break;
+        const uint4 v = pieces[row * 8 + ((lane & 7) ^ (row & 7))];
+        if (col + kPiece <= cols) {
+            __stcs(reinterpret_cast<uint4 *>(at), v);
+        } else {
+            const T *e = reinterpret_cast<const T *>(&v);
+#pragma unroll
+            for (int k = 0; k < kPiece; ++k)
+                if (col + k < cols) at[k] = e[k];
+        }
     }
 }
-// Any other 32 columns of a warp's 32 rows (lane = row), turned through shared memory so that a store takes neighbours.
+// 32 columns of rows that are not aligned, element by element.
 template <typename T>
 __device__ __forceinline__ void store_turned(T *first, long long ld, int rows, int cols, const uint32_t *w, float *turn)
 {
@@ -474,18 +494,19 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
         for (long long t = first; t < tiles && ok; t += stride, ++round) {
             const PairTile p = pair_tile(g, t, 0);
             const uint32_t desc = mma_desc(256, p.cols, 0);
+            const uint32_t sums = tmem + pair_sums_at(round);
             if (round > 0 && !warp_wait(smem_addr(&sh->sums_empty), (round - 1) & 1u, gave_up, g.limit)) break;
             for (int k = 0; k < g.tiles_k; ++k) {
                 // both blocks' copies have landed and their scales are in tensor memory
                 if (!(ok = warp_wait(smem_addr(&sh->scaled[s]), parity, gave_up, g.limit))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t base_a = smem_addr(ring + s * kPairStageBytes), base_b = base_a + kMxTileBytes + 2 * kMxScaleBytes;
-                const uint32_t sf = tmem + 256 + s * kPairScaleColumns;
+                const uint32_t sf = tmem + 256 + kPairOverlap + s * kPairScaleColumns;
                 const uint64_t da = codes_desc(base_a + kMxScaleBytes), db = codes_desc(base_b);
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     if (4 * k + q < g.k_steps)
-                        mma_mx4<true>(one, tmem, da + 2 * q, db + 2 * q, desc | (q & 1 ? mma_desc(0, 0, 2) : 0), sf + (q >> 1) * 4,
+                        mma_mx4<true>(one, sums, da + 2 * q, db + 2 * q, desc | (q & 1 ? mma_desc(0, 0, 2) : 0), sf + (q >> 1) * 4,
                                       sf + 8 + (q >> 1) * 8, k > 0 || q > 0);
                 commit_pair(one, smem_addr(&sh->empty[s]));
                 if (++s == kPairStages) {
@@ -518,7 +539,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
                     v[4 * i + 2] = w[i].z;
                     v[4 * i + 3] = w[i].w;
                 }
-                const uint32_t sf = tmem + ((uint32_t)(quarter * 32) << 16) + 256 + s * kPairScaleColumns;
+                const uint32_t sf = tmem + ((uint32_t)(quarter * 32) << 16) + 256 + kPairOverlap + s * kPairScaleColumns;
                 store_columns8(sf, v);
                 store_columns8(sf + 8, v + 8);
                 store_columns8(sf + 16, v + 16);
@@ -543,35 +564,36 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
             const PairTile p = pair_tile(g, t, rank);
             if (!__all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->sums_full), round & 1u, gave_up, g.limit))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            // Batches of columns kept for after the release, as many as the registers hold; the others are stored at once.
-            constexpr int kKept = sizeof(T) == 4 ? 2 : 3;
             const int here = p.rows - quarter * 32 < 32 ? p.rows - quarter * 32 : 32;       // of this warp's rows
             T *corner = static_cast<T *>(g.out) + (p.i0 + quarter * 32) * g.ld + p.j0;
-            auto store = [&](int c, const uint32_t *w) {
-                const int col = half * 128 + c * 32, have = (int)(g.n - p.j0 - col < 32 ? g.n - p.j0 - col : 32);
-                if (have <= 0 || here <= 0) return;
-                if (g.vec && have == 32) {
-                    if (lane < here) store_row32<T>(corner + lane * g.ld + col, g.vec, w);
-                } else {
-                    store_turned<T>(corner + col, g.ld, here, have, w, turn);
-                }
-            };
-            uint32_t w[kKept][32 * sizeof(T) / 4];
+            // First the half of the columns that the next tile's sums will lie in, then the other.
+            const int shared = pair_sums_at(round + 1);
+            const uint32_t sums = tmem + ((uint32_t)(quarter * 32) << 16) + pair_sums_at(round);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[32];
-                load_columns32(tmem + ((uint32_t)(quarter * 32) << 16) + half * 128 + c * 32, v);
+            for (int pass = 0; pass < 2; ++pass) {
+                const int col = (pass == 0 ? shared : kPairOverlap - shared) + half * 64;
+                constexpr int kWords = 32 * (int)sizeof(T) / 4;       // of 32 columns
+                uint32_t v[64], w[2 * kWords];
+                load_columns32(sums + col, v);
+                load_columns32(sums + col + 32, v + 32);
                 columns_loaded();
-                const int at = c < 4 - kKept ? 0 : c - (4 - kKept);
-                round32<T>(v, w[at]);
-                if (c < 4 - kKept) store(c, w[at]);
-            }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            // Nothing written here is for the partner: a release would wait for the last tile's stores.
-            if (lane == 0) mbar_tell(smem_addr(&sh->sums_empty), 0);
+                round32<T>(v, w);
+                round32<T>(v + 32, w + kWords);
+                if (pass == 0) {
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    // Nothing written here is for the partner: a release would wait for the last tile's stores.
+                    if (lane == 0) mbar_tell(smem_addr(&sh->sums_empty), 0);
+                }
+                constexpr int kAtOnce = 128 / (int)sizeof(T);
+                const int have = (int)(g.n - p.j0 - col < 64 ? g.n - p.j0 - col : 64);
 #pragma unroll
-            for (int c = 4 - kKept; c < 4; ++c) store(c, w[c - (4 - kKept)]);
+                for (int c = 0; c < 64; c += 32) {
+                    if (c >= have) break;
+                    if (!g.vec) store_turned<T>(corner + col + c, g.ld, here, have - c, w + c * (int)sizeof(T) / 4, turn);
+                    else if (c % kAtOnce == 0) store_lines<T>(corner + col + c, g.ld, here, have - c, w + c * (int)sizeof(T) / 4, turn);
+                }
+            }
         }
     }
     __syncwarp();
@@ -837,7 +859,7 @@ extern "C" zoa_status zoa_mx4_matmul(const void *a, const void *b, size_t m, siz
     g.tiles_k = (int)mx_tiles((long long)k, kMxTileCols);
     g.k_steps = (int)mx_tiles((long long)k, 64);
     const size_t row_bytes = ld * dtype_bytes(dtype), at = reinterpret_cast<uintptr_t>(out);
-    g.vec = (at | row_bytes) % 32 == 0 ? 2 : (at | row_bytes) % 16 == 0 ? 1 : 0;
+    g.vec = (at | row_bytes) % 16 == 0;
     g.test_stop = ops_test_stop();
     g.limit.error_word = ops_error_word();
     g.limit.ns = ops_wait_limit_ns();
