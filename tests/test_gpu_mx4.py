@@ -206,6 +206,19 @@ def test_linear_training_step(tokens, k, n, dtype):
     assert torch.equal(ya, y) and torch.equal(xa.grad, dx) and torch.equal(wa.grad, dw)
 
 
+@pytest.mark.parametrize("tokens,k,n,dtype", [(600, 1500, 2100, torch.bfloat16), (3000, 2000, 2500, torch.float16), (300, 5000, 260, torch.bfloat16),
+                                              (2600, 257, 4900, torch.float32), (1, 700, 900, torch.float16), (1029, 1001, 1333, torch.float32)])
+def test_both_gradients_at_once(tokens, k, n, dtype):
+    """The two products of the backward pass share a launch; fewer tiles than pairs of SMs, more, and uneven rests."""
+    x, w, dy = data(tokens, k, dtype, 1, 0.5), data(n, k, dtype, 2, 0.1, 0.05), data(tokens, n, dtype, 3, 0.5, 0.01)
+    y, saved = mx4_linear_forward(x, w)
+    dx, dw = mx4_linear_backward(dy, saved)
+    assert_product(dx, round_mx4(as64(dy)), round_mx4(as64(w).T), dtype)
+    assert_product(dw, round_mx4(as64(dy).T), round_mx4(as64(x).T), dtype)
+    again = mx4_linear_backward(dy, saved)
+    assert torch.equal(dx, again[0]) and torch.equal(dw, again[1])
+
+
 def test_linear_gradient_against_differences_on_the_grid():
     """With inputs on the 4-bit grid in both directions the layer is bilinear, so differences are its gradient."""
     g = torch.Generator().manual_seed(9)
@@ -368,6 +381,27 @@ def test_a_wait_that_runs_out_is_reported(m, n):
         B.zoa_ops_set_option(B.OPT_TEST_STOP_AFTER_TILES, 0)
     B.zoa_ops_check_device()
     assert_product(mx4_matmul(a, b), round_mx4(as64(x)), round_mx4(as64(w)), torch.bfloat16)
+
+
+def test_a_wait_that_runs_out_in_both_gradients_is_reported():
+    x, w = data(2000, 1500, torch.bfloat16, 1, 0.5), data(1300, 1500, torch.bfloat16, 2, 0.1, 0.05)
+    dy = data(2000, 1300, torch.bfloat16, 3, 0.5, 0.01)
+    y, saved = mx4_linear_forward(x, w)
+    want = mx4_linear_backward(dy, saved)
+    B.zoa_ops_check_device()
+    try:
+        B.zoa_ops_set_option(B.OPT_WAIT_LIMIT_MS, 20)
+        B.zoa_ops_set_option(B.OPT_TEST_STOP_AFTER_TILES, 3)
+        mx4_linear_backward(dy, saved)
+        with pytest.raises(ZoaError) as e:
+            B.zoa_ops_check_device()
+        assert e.value.status == B.ERR_DEVICE
+    finally:
+        B.zoa_ops_set_option(B.OPT_WAIT_LIMIT_MS, 2000)
+        B.zoa_ops_set_option(B.OPT_TEST_STOP_AFTER_TILES, 0)
+    B.zoa_ops_check_device()
+    got = mx4_linear_backward(dy, saved)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 def test_structure_sizes_match_the_header():
