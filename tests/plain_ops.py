@@ -70,6 +70,8 @@ def distill(z, index, teacher, labels=None, weight=None, lse=None, temperature=1
                 if p_rest > 0 and q_rest > 1e-30:
                     soft += p_rest * (np.log(p_rest) - np.log(q_rest))
                     d[out] -= p_rest * q[out] / q_rest
+                else:                    # a term that is left out has no derivative
+                    d -= p_rest * q
             loss[r] += soft_weight * T * T * soft
             grad[r] += soft_weight * T * d
         if labels is not None and 0 <= labels[r] < vocab:

@@ -55,3 +55,33 @@ def test_gradient_against_differences(tail, hard, T):
         diff = (distill(up, index, teacher, **args)[0] - distill(down, index, teacher, **args)[0]) / (2 * h)
         # central differences: an error of h^2 / 6 times a third derivative below 10, and 2^-52 * loss / h of rounding
         assert np.abs(diff - grad[:, j]).max() < 1e-9 + 2e-10
+
+
+@pytest.mark.parametrize("T", [0.5, 1.0, 2.0])
+@pytest.mark.parametrize("unlisted", ["masked", "none"])
+def test_gradient_against_differences_without_unlisted_mass(unlisted, T):
+    """The teacher's own log-sum-exp, and no unlisted token that the student can choose: the term of the rest is left out
+    of the loss, and so of its derivative."""
+    rng = np.random.default_rng(6)
+    rows, top = 3, 4
+    vocab = 11 if unlisted == "masked" else top
+    z = rng.standard_normal((rows, vocab))
+    index = np.stack([rng.permutation(vocab)[:top] for _ in range(rows)])
+    if unlisted == "masked":
+        kept = np.take_along_axis(z, index, 1)
+        z[:] = -np.inf
+        np.put_along_axis(z, index, kept, 1)
+    teacher = rng.standard_normal((rows, top))
+    args = dict(lse=np.log(np.exp(teacher / T).sum(1)) + 0.3, temperature=T, soft_weight=0.7)
+    _, grad = distill(z, index, teacher, **args)
+    # central differences, as above
+    h = 1e-5
+    for r in range(rows):
+        for j in index[r]:
+            up, down = z[r:r + 1].copy(), z[r:r + 1].copy()
+            up[0, j] += h
+            down[0, j] -= h
+            one = dict(args, lse=args["lse"][r:r + 1])
+            diff = (distill(up, index[r:r + 1], teacher[r:r + 1], **one)[0] - distill(down, index[r:r + 1], teacher[r:r + 1], **one)[0]) / (2 * h)
+            assert abs(diff[0] - grad[r, j]) < 1e-9 + 2e-10
+    assert np.abs(grad.sum(1)).max() < 1e-12        # a distribution less a distribution of the same mass
