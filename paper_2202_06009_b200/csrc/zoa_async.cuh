@@ -80,19 +80,26 @@ __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, const 
     const unsigned long long start = timer_ns();
     while (!mbar_try(bar, parity) && timer_ns() - start < limit.ns) {}
 }
+// The same place in the shared memory of block `rank` of this cluster.
+__device__ __forceinline__ uint32_t address_at(uint32_t addr, uint32_t rank)
+{
+    uint32_t remote;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+    return remote;
+}
 // Arrives on the barrier at the same place in block `rank` of this cluster.
 __device__ __forceinline__ void mbar_arrive_at(uint32_t bar, uint32_t rank)
 {
-    uint32_t remote;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(bar), "r"(rank));
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(address_at(bar, rank)) : "memory");
 }
-// The same without ordering this thread's own earlier writes, which a release at cluster scope waits for.
+// The same without ordering any of this thread's earlier accesses to memory: for tensor memory alone, whose own fences order it.
 __device__ __forceinline__ void mbar_tell(uint32_t bar, uint32_t rank)
 {
-    uint32_t remote;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(bar), "r"(rank));
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(address_at(bar, rank)) : "memory");
+}
+__device__ __forceinline__ void store_there(uint32_t addr, uint32_t rank, int v)
+{
+    asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(address_at(addr, rank)), "r"(v) : "memory");
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {

@@ -1,0 +1,51 @@
+"""The 4-bit layer's calls in the forms and at the sizes where they can go wrong: rests of the large product's tiles, operands that
+change under repeated calls, gradients that autograd makes, empty sizes, mixed types, one-sided gradients, refusals.
+Tolerances are test_gpu_mx4.assert_product's."""
+import pytest
+import torch
+
+from paper_2202_06009_b200 import mx4_matmul, mx4_quantize
+from test_gpu_mx4 import ULP, data
+
+pytestmark = pytest.mark.gpu
+
+
+def assert_product_on_gpu(got, a, b, dtype):
+    """test_gpu_mx4.assert_product for large results, in 64 bits on the GPU; a, b: the values of the forms."""
+    a, b = a.double(), b.double()
+    want, size = a @ b.t(), a.abs() @ b.abs().t()
+    rel, least = ULP[dtype]
+    bound = (a.shape[1] / 8 + 8) * 2.0 ** -23 * size + rel * want.abs() + least
+    assert ((got.double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rest", [1, 16, 33, 64, 100, 128, 129, 161, 200, 255])
+def test_large_product_with_a_rest(rest, dtype):
+    """Rows and columns of the last tiles of 256 from one to all but one; each block of a pair brings its own part."""
+    k = 1100 + rest
+    for m, n in ((2304, 2048 + rest), (2048 + rest, 2304), (2304 + rest, 2304 + rest)):
+        a, b = data(m, k, torch.bfloat16, rest, 0.5), data(n, k, torch.bfloat16, rest + 1, 0.5, 0.1)
+        qa, qb = mx4_quantize(a), mx4_quantize(b)
+        assert_product_on_gpu(mx4_matmul(qa, qb, dtype), qa.dequantize(torch.float32), qb.dequantize(torch.float32), dtype)
+
+
+@pytest.mark.parametrize("m,n,k", [(2304, 2304, 4096), (4096, 2049, 900), (9000, 700, 300)])
+def test_large_products_of_operands_that_change(m, n, k):
+    """Each call's operands replace the last call's in the same buffers: a product that began before a block's copies
+    had landed would find old ones."""
+    sets = [(data(m, k, torch.bfloat16, 10 * i, 0.5), data(n, k, torch.bfloat16, 10 * i + 1, 0.5, 0.1)) for i in range(2)]
+    qa, qb = mx4_quantize(sets[0][0]), mx4_quantize(sets[0][1])
+    want = []
+    for a, b in sets:
+        mx4_quantize(a, out=qa)
+        mx4_quantize(b, out=qb)
+        want.append(mx4_matmul(qa, qb, torch.float32))
+        assert_product_on_gpu(want[-1], qa.dequantize(torch.float32), qb.dequantize(torch.float32), torch.float32)
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for i in range(60):
+        a, b = sets[i % 2]
+        mx4_quantize(a, out=qa)
+        mx4_quantize(b, out=qb)
+        wrong += (mx4_matmul(qa, qb, torch.float32) != want[i % 2]).sum()
+    assert wrong.item() == 0
