@@ -330,6 +330,13 @@ __global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_ke
         else list[k].first = mine(i);
     }
     __syncthreads();
+    if (sh.twice)         // the earliest entry of a token counts as its first, whichever thread came first: equal calls add in equal order
+        for (int k = tid; k < a.top; k += kThreads) {
+            const int i = list[k].token;
+            bool first = i >= 0 && mine(i);
+            for (int o = 0; o < k && first; ++o) first = list[o].token != i;
+            list[k].first = first;
+        }
     if (warp == kWarps - 1) {          // the teacher's probabilities, by one warp beside the others' sums
         float high = -INFINITY;
         bool some = false;

@@ -32,3 +32,24 @@ def test_gradient_without_unlisted_mass(rows, vocab, top, T, dtype):
     if dtype == torch.float32:
         g = grad.double()         # the entries' tolerances together
         assert (g.sum(1).abs() <= 4e-5 * (g.abs().sum(1) + 2 * 0.7 * T)).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab,top", [(300, 2000, 256), (3, 30522, 64), (40, 700, 512)])
+def test_tokens_listed_twice_give_equal_bits(rows, vocab, top, dtype):
+    """A token's share counts once, and the same entry's thread adds it in every call."""
+    p = problem(rows, vocab, top, dtype, 14, tail=True, labels=True, T=1.5)
+    p["row_weight"] = None
+    half = top // 2
+    p["index"][:, half:] = p["index"][:, :half].roll(5, 1)
+    p["teacher_lse"] += 1.0
+    loss, stats = distill_topk(**p, stats=True)
+    check(p, loss)
+    both, grad = distill_topk_grad(**p)
+    check(p, both, grad)
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(50):
+        again, stats2 = distill_topk(**p, stats=True)
+        both2, grad2 = distill_topk_grad(**p)
+        wrong += (again != loss).sum() + (stats2 != stats).sum() + (both2 != both).sum() + (grad2 != grad).sum()
+    assert wrong.item() == 0
