@@ -346,19 +346,20 @@ __global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_ke
                 high = fmaxf(high, list[k].p);
             }
         int any = __any_sync(0xffffffffu, some);
+        // log p = (logit - high) / T - log_norm: without the largest taken off first, logits far from zero would lose their digits
         float log_norm = a.lse ? a.lse[row] : 0.0f;
+        high = a.lse ? 0.0f : base_of(warp_max(high));
         if (!a.lse) {
-            high = base_of(warp_max(high));
             float sum = 0.0f;
             for (int k = lane; k < a.top; k += 32)
                 if (list[k].token >= 0) sum += ex2((list[k].p - high) * c);
             sum = warp_sum(sum);
             if (sum == 0.0f) any = 0;            // a list of -inf says nothing
-            log_norm = any ? logf(sum) + high * inv_t : 0.0f;
+            log_norm = any ? logf(sum) : 0.0f;
         }
         float mass = 0.0f, soft = 0.0f;
         for (int k = lane; k < a.top; k += 32) {
-            const float log_p = list[k].p * inv_t - log_norm;
+            const float log_p = (list[k].p - high) * inv_t - log_norm;
             const float p = list[k].token >= 0 && any ? ex2(log_p * kLog2e) : 0.0f;
             list[k].p = p;
             mass += p;

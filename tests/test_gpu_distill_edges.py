@@ -53,3 +53,13 @@ def test_tokens_listed_twice_give_equal_bits(rows, vocab, top, dtype):
         both2, grad2 = distill_topk_grad(**p)
         wrong += (again != loss).sum() + (stats2 != stats).sum() + (both2 != both).sum() + (grad2 != grad).sum()
     assert wrong.item() == 0
+
+
+@pytest.mark.parametrize("T", [0.25, 1.0, 3.0])
+@pytest.mark.parametrize("far", [-40000.0, 700.0, 50000.0])
+def test_teacher_logits_far_from_zero(far, T):
+    """A softmax does not depend on where its logits lie: the same tolerances as near zero."""
+    p = problem(9, 300, 12, torch.float32, 13, labels=True, T=T)
+    p["row_weight"] = None
+    p["teacher"] += far
+    check(p, *distill_topk_grad(**p))
