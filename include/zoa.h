@@ -492,7 +492,8 @@ zoa_status zoa_mx4_linear_backward(const void *dy, int dy_type, size_t ld_dy, si
  * no hard part.  A row of weight 0 gives loss 0 and gradient 0 whatever it holds.
  * Logits of -inf are tokens masked out (q = 0, gradient 0); a row of nothing else
  * gives loss 0 and gradient 0.  The p_r term is left out of a row whose q_r is 0 or
- * below 1e-30.  A NaN or +inf logit makes its row NaN.  All sums in binary32; the
+ * below 1e-30.  A NaN or +inf logit makes its row NaN, and so
+ * does a NaN among the listed teacher's logits.  All sums in binary32; the
  * order of a row's sums depends on the sizes of the call, the alignment of its
  * rows and the outputs asked for (a loss alone and one beside a gradient may differ
  * in their last bits): equal calls give equal bits.  Limits: vocab in

@@ -518,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_ke
     if (grad) {
         const float c0 = any ? w * a.soft_weight * a.temperature : 0.0f;
         // (a row whose loss has no term of the rest has none in its gradient)
-        const float ca = empty ? 0.0f : c0 * (a.lse ? mass + (rest ? p_rest : 0.0f) : 1.0f) / t.s;
+        const float ca = empty ? 0.0f : c0 * (a.lse || mass != mass ? mass + (rest ? p_rest : 0.0f) : 1.0f) / t.s;
         const float cu = rest && !empty ? ca - c0 * p_rest / t.r : ca;
         const float ch = hard ? w * a.hard_weight : 0.0f;
         const float cb = empty ? 0.0f : ch / t.s1;

@@ -63,3 +63,26 @@ def test_teacher_logits_far_from_zero(far, T):
     p["row_weight"] = None
     p["teacher"] += far
     check(p, *distill_topk_grad(**p))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("vocab,top", [(60, 8), (9000, 100)])
+def test_nan_among_the_teachers_logits(vocab, top, tail, dtype):
+    """It makes its row NaN, loss and gradient; in a skipped entry, or in a row of weight 0, it is not looked at."""
+    p = problem(9, vocab, top, dtype, 12, tail=tail, labels=True, T=2.0)
+    p["row_weight"] = torch.ones(9, device="cuda")
+    p["teacher"][1, 0], p["teacher"][2, top - 1] = float("nan"), float("nan")
+    p["teacher"][3, 1] = float("nan")
+    p["index"][3, 1] = -1
+    p["teacher"][5] = float("nan")
+    p["row_weight"][5] = 0
+    others = [0, 3, 4, 5, 6, 7, 8]
+    q = {k: v[others] if isinstance(v, torch.Tensor) else v for k, v in p.items()}
+    both, grad = distill_topk_grad(**p)
+    loss, stats = distill_topk(**p, stats=True)
+    back = distill_topk_backward(torch.ones(9, device="cuda"), stats, **p)
+    for got in (both, loss, grad, back):
+        assert torch.isnan(got[1:3]).all()
+    check(q, both[others], grad[others])
+    check(q, loss[others], back[others], np.ones(7))
