@@ -497,7 +497,7 @@ zoa_status zoa_mx4_linear_backward(const void *dy, int dy_type, size_t ld_dy, si
  * order of a row's sums depends on the sizes of the call, the alignment of its
  * rows and the outputs asked for (a loss alone and one beside a gradient may differ
  * in their last bits): equal calls give equal bits.  Limits: vocab in
- * [1, 2^20], top in [1, 2048].
+ * [1, 2^20], top in [1, 2048], T in [2^-126, infinity).
  * zoa_distill_topk: loss (binary32 [rows], may be NULL), and, where they are not
  * NULL, grad [rows, vocab] (the logits' type; may be the logits themselves with the
  * same ld: they are then replaced) and stats (binary32 [rows, 4], 16-byte aligned, for

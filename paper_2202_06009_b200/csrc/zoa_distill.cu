@@ -8,6 +8,7 @@
 #include "zoa_async.cuh"
 #include "zoa_ops.h"
 
+#include <cfloat>
 #include <type_traits>
 
 namespace zoa {
@@ -611,7 +612,8 @@ zoa_status launch(const char *me, const zoa_distill_args *x, const float *stats_
     if (x->top < 1 || x->top > kMaxTop) return ops_fail(ZOA_ERR_ARG, "%s: top must be in [1, 2048]", me);
     if (x->rows > ((size_t)1 << 31) - 1) return ops_fail(ZOA_ERR_ARG, "%s: at most 2^31 - 1 rows", me);
     if (x->ld_logits < x->vocab || (grad && ld_grad < x->vocab)) return ops_fail(ZOA_ERR_ARG, "%s: ld must be at least vocab", me);
-    if (!(x->temperature > 0.0f) || x->temperature * 0.0f != 0.0f) return ops_fail(ZOA_ERR_ARG, "%s: temperature must be positive and finite", me);
+    if (!(x->temperature >= FLT_MIN) || x->temperature * 0.0f != 0.0f)      // so that 1 / T and its product with log2 e are finite
+        return ops_fail(ZOA_ERR_ARG, "%s: temperature must be positive, finite and not subnormal", me);
     if (!(x->soft_weight * 0.0f == 0.0f) || !(x->hard_weight * 0.0f == 0.0f))
         return ops_fail(ZOA_ERR_ARG, "%s: soft_weight and hard_weight must be finite", me);
     if (x->rows == 0) return ZOA_OK;

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2202_06009_b200 import distill_topk, distill_topk_backward, distill_topk_grad
+from paper_2202_06009_b200 import ZoaError, binding as B, distill_topk, distill_topk_backward, distill_topk_grad
 from test_gpu_distill import TYPES, check, problem
 
 pytestmark = pytest.mark.gpu
@@ -86,3 +86,21 @@ def test_nan_among_the_teachers_logits(vocab, top, tail, dtype):
         assert torch.isnan(got[1:3]).all()
     check(q, both[others], grad[others])
     check(q, loss[others], back[others], np.ones(7))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tail,labels,T", [(False, False, 0.5), (True, True, 0.5), (True, True, 0.1), (False, True, 0.02), (True, False, 0.1)])
+@pytest.mark.parametrize("rows,vocab,top", [(5, 33, 40), (9, 1000, 8), (4, 30522, 32)])
+def test_temperatures_below_one(rows, vocab, top, tail, labels, T, dtype):
+    p = problem(rows, vocab, top, dtype, rows + top, tail=tail, labels=labels, T=T)
+    check(p, *distill_topk_grad(**p))
+
+
+def test_temperatures_whose_reciprocal_overflows_are_refused():
+    p = problem(4, 50, 6, torch.float32, 1)
+    for T in (1e-39, 1e-45, 2.0 ** -127):
+        with pytest.raises(ZoaError) as e:
+            distill_topk(**dict(p, temperature=T))
+        assert e.value.status == B.ERR_ARG
+    loss = distill_topk(**dict(p, temperature=1e-30))
+    assert not torch.isnan(loss).any()
