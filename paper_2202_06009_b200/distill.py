@@ -7,7 +7,7 @@ import struct
 import torch
 
 from . import binding as B
-from .mx4 import _call, _check_result, _matrix
+from .mx4 import _call, _check_result, _matrix, _only_first
 
 _lib = B.lib
 _pack = struct.Struct("@6P4Ni3f").pack          # zoa_distill_args
@@ -95,4 +95,5 @@ class DistillTopkFunction(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_loss):
-        return distill_topk_backward(grad_loss.contiguous(), *ctx.saved_tensors, **ctx.options), None, None, None
+        grad, = _only_first(distill_topk_backward(grad_loss.contiguous(), *ctx.saved_tensors, **ctx.options))
+        return grad, None, None, None

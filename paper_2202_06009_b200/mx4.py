@@ -205,6 +205,23 @@ def mx4_linear_backward(dy, saved, need_dx=True, need_dw=True):
     return dx, dw
 
 
+class _OnlyFirst(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, grad, anchor):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("a second derivative through Mx4LinearFunction or DistillTopkFunction is not offered")
+
+
+def _only_first(*grads):
+    """Gradients that refuse to be differentiated (under create_graph), instead of passing for constants."""
+    if not torch.is_grad_enabled():
+        return grads
+    return tuple(g if g is None else _OnlyFirst.apply(g, torch.empty(0, requires_grad=True)) for g in grads)
+
+
 class Mx4LinearFunction(torch.autograd.Function):
     """mx4_linear_forward / mx4_linear_backward under autograd: y = Mx4LinearFunction.apply(x, w)."""
 
@@ -218,4 +235,4 @@ class Mx4LinearFunction(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         saved = Mx4LinearSaved(ctx.saved_tensors[0], *ctx.layer)
-        return mx4_linear_backward(dy if dy.stride(-1) == 1 else dy.contiguous(), saved, *ctx.needs_input_grad)
+        return _only_first(*mx4_linear_backward(dy if dy.stride(-1) == 1 else dy.contiguous(), saved, *ctx.needs_input_grad))
