@@ -82,6 +82,9 @@ def distill_topk_backward(grad_loss, stats, logits, index, teacher, *, labels=No
     return grad
 
 
+_TENSORS = ("labels", "row_weight", "teacher_lse")      # of distill_topk's options
+
+
 class DistillTopkFunction(torch.autograd.Function):
     """distill_topk under autograd (by the logits): DistillTopkFunction.apply(logits, index, teacher, options) with
     options a dict of distill_topk's keyword arguments."""
@@ -89,11 +92,14 @@ class DistillTopkFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, index, teacher, options):
         loss, stats = distill_topk(logits, index, teacher, stats=True, **options)
-        ctx.options = options
-        ctx.save_for_backward(stats, logits, index, teacher)
+        # tensors among the options are kept as the others are, so that changing one before the backward pass is noticed
+        ctx.numbers = {name: value for name, value in options.items() if name not in _TENSORS}
+        ctx.save_for_backward(stats, logits, index, teacher, *(options.get(name) for name in _TENSORS))
         return loss
 
     @staticmethod
     def backward(ctx, grad_loss):
-        grad, = _only_first(distill_topk_backward(grad_loss.contiguous(), *ctx.saved_tensors, **ctx.options))
+        *inputs, labels, row_weight, teacher_lse = ctx.saved_tensors
+        grad, = _only_first(distill_topk_backward(grad_loss.contiguous(), *inputs, labels=labels, row_weight=row_weight,
+                                                  teacher_lse=teacher_lse, **ctx.numbers))
         return grad, None, None, None

@@ -21,3 +21,16 @@ def test_a_second_derivative_is_refused():
     for g, t in ((dx, x), (dw, w)):
         with pytest.raises(RuntimeError):
             ((g * g).sum() + t.sum()).backward()
+
+
+@pytest.mark.parametrize("what", ["labels", "row_weight", "teacher_lse", "index", "teacher", "logits"])
+def test_inputs_changed_before_the_backward_pass_are_noticed(what):
+    p = problem(6, 50, 6, torch.float32, 2, tail=True, labels=True, T=2.0)
+    options = {k: v for k, v in p.items() if k not in ("logits", "index", "teacher")}
+    z = p["logits"].clone().requires_grad_()
+    leaf = z * 1.0
+    loss = DistillTopkFunction.apply(leaf, p["index"], p["teacher"], options)
+    with torch.no_grad():
+        (leaf if what == "logits" else p[what]).add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.sum().backward()
