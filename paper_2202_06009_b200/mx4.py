@@ -13,6 +13,7 @@ _current_device = torch.cuda.current_device
 _raw_stream = torch._C._cuda_getCurrentRawStream      # of a device's current stream, without the Stream object around it
 _TILE_ROWS, _TILE_COLS, _TILE_BYTES = 128, 256, B.zoa_mx4_size(1, 1)
 _MAX_SIDE = 1 << 30
+_changed = torch.autograd.graph.increment_version
 
 
 def _matrix(x, what):
@@ -32,9 +33,13 @@ def _matrix(x, what):
 
 
 def _check_result(out, rows, cols, dtype, device, what="out"):
+    """The row distance of a tensor that a call will write into, which autograd is told of: a node that kept the tensor
+    must not use what it then holds."""
     if out.shape != (rows, cols) or out.dtype != dtype or out.device != device:
         raise ValueError(f"{what} must be a {dtype} tensor of shape ({rows}, {cols}) on {device}")
-    return _matrix(out, what)[3]
+    ld = _matrix(out, what)[3]
+    _changed(out)
+    return ld
 
 
 def _call(fn, device, *args):
@@ -101,6 +106,7 @@ def _form(out, rows, cols, device, what):
         return Mx4(rows, cols, device)
     if out.shape != (rows, cols) or out.device != device:
         raise ValueError(f"{what} must be an Mx4 of shape ({rows}, {cols}) on {device}")
+    _changed(out.data)
     return out
 
 

@@ -2,7 +2,8 @@
 import pytest
 import torch
 
-from paper_2202_06009_b200 import DistillTopkFunction, Mx4LinearFunction
+from paper_2202_06009_b200 import (DistillTopkFunction, Mx4LinearFunction, distill_topk, distill_topk_backward, distill_topk_grad, mx4_linear,
+                                   mx4_matmul, mx4_quantize)
 from test_gpu_distill import problem
 
 pytestmark = pytest.mark.gpu
@@ -34,3 +35,30 @@ def test_inputs_changed_before_the_backward_pass_are_noticed(what):
         (leaf if what == "logits" else p[what]).add_(1)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.sum().backward()
+
+
+def test_results_written_over_saved_tensors_are_noticed():
+    """`out` counts as a change in place: a node that kept the tensor refuses its backward pass."""
+    p = problem(6, 64, 6, torch.float32, 2)
+    x = torch.randn(6, 64, device="cuda")
+    q = mx4_quantize(x)
+    square = mx4_quantize(torch.randn(64, 64, device="cuda"))
+    stats = distill_topk(**p, stats=True)[1]
+
+    def writes(h):
+        z = dict(p, logits=h)
+        yield lambda: distill_topk_grad(**z, out=h)
+        yield lambda: distill_topk_backward(torch.ones(6, device="cuda"), stats, **p, out=h)
+        yield lambda: q.dequantize(torch.float32, out=h)
+        yield lambda: mx4_matmul(q, square, torch.float32, out=h)
+        yield lambda: mx4_linear(x, square, out=h)
+
+    for i in range(5):
+        a = torch.randn(6, 64, device="cuda").requires_grad_()
+        kept = torch.exp(a)                  # its backward pass needs its result
+        list(writes(kept.detach()))[i]()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            kept.sum().backward()
+    with torch.inference_mode():
+        assert distill_topk_grad(**p, out=torch.empty(6, 64, device="cuda"))[1].shape == (6, 64)
+        assert mx4_linear(x, square, out=torch.empty(6, 64, device="cuda")).shape == (6, 64)
