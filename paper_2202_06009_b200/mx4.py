@@ -241,4 +241,7 @@ class Mx4LinearFunction(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         saved = Mx4LinearSaved(ctx.saved_tensors[0], *ctx.layer)
-        return _only_first(*mx4_linear_backward(dy if dy.stride(-1) == 1 else dy.contiguous(), saved, *ctx.needs_input_grad))
+        ld, step = dy.stride()
+        if step != 1 or ld < dy.shape[1]:       # transposed, or broadcast (a sum over tokens hands back one row for all)
+            dy = dy.contiguous()
+        return _only_first(*mx4_linear_backward(dy, saved, *ctx.needs_input_grad))

@@ -4,7 +4,7 @@ Tolerances are test_gpu_mx4.assert_product's."""
 import pytest
 import torch
 
-from paper_2202_06009_b200 import mx4_matmul, mx4_quantize
+from paper_2202_06009_b200 import Mx4LinearFunction, mx4_linear_backward, mx4_linear_forward, mx4_matmul, mx4_quantize
 from test_gpu_mx4 import ULP, data
 
 pytestmark = pytest.mark.gpu
@@ -49,3 +49,20 @@ def test_large_products_of_operands_that_change(m, n, k):
         mx4_quantize(b, out=qb)
         wrong += (mx4_matmul(qa, qb, torch.float32) != want[i % 2]).sum()
     assert wrong.item() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,k,n", [(1, 64, 48), (50, 100, 70), (300, 256, 1), (3, 33, 129)])
+def test_gradients_that_autograd_broadcasts(tokens, k, n, dtype):
+    """Sums and means over tokens, outputs or both hand back expanded tensors, some of whose strides are 0."""
+    x, w = data(tokens, k, dtype, 1, 0.5), data(n, k, dtype, 2, 0.1, 0.05)
+    v, u = data(1, n, dtype, 3)[0], data(1, tokens, dtype, 4)[0]
+    losses = [lambda y: (y.sum(0) * v).sum(), lambda y: (y.mean(0) * v).sum(), lambda y: (y.sum(1) * u).sum(), lambda y: y.sum(),
+              lambda y: ((y + v).sum(0) * v).sum(), lambda y: y.t().sum(0).sum(), lambda y: (y.t() @ u).sum()]
+    for loss in losses:
+        xa, wa = x.clone().requires_grad_(), w.clone().requires_grad_()
+        y = Mx4LinearFunction.apply(xa, wa)
+        y.retain_grad()
+        loss(y).backward()
+        dx, dw = mx4_linear_backward(y.grad.contiguous(), mx4_linear_forward(x, w)[1])
+        assert torch.equal(xa.grad, dx) and torch.equal(wa.grad, dw)
