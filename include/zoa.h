@@ -464,7 +464,7 @@ zoa_status zoa_mx4_linear(const void *x, int dtype, size_t m, size_t k, size_t l
  * y) and w [n, k]; xt and wt receive the forms of x^T (zoa_mx4_size(k, m) bytes) and w^T
  * (zoa_mx4_size(k, n)) for the next call; work: (device) zoa_mx4_size(m, k) + zoa_mx4_size(n, k) bytes.
  * zoa_mx4_linear_backward: dx [m, k] = Q(dy) Q(w^T)^T and dw [n, k] = Q(dy^T) Q(x^T)^T from
- * dy [m, n]; either may be NULL if it is not wanted; work: (device) zoa_mx4_size(m, n) +
+ * dy [m, n]; either may be NULL if it is not wanted, or has no elements; work: (device) zoa_mx4_size(m, n) +
  * zoa_mx4_size(n, m) bytes.  All forms and work areas 16-byte aligned. */
 zoa_status zoa_mx4_linear_forward(const void *x, int x_type, size_t ldx, const void *w, int w_type, size_t ldw, size_t m,
                                   size_t n, size_t k, void *y, size_t ldy, void *xt, void *wt, void *work, void *stream);

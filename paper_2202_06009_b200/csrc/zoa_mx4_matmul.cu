@@ -1111,10 +1111,10 @@ extern "C" zoa_status zoa_mx4_linear_backward(const void *dy, int dy_type, size_
                                               void *work, void *stream)
 {
     const char *me = "zoa_mx4_linear_backward";
-    if (!dx && !dw) return ops_fail(ZOA_ERR_ARG, "%s: neither dx nor dw is asked for", me);
-    if (m && n && !work) return ops_fail(ZOA_ERR_ARG, "%s: work is NULL", me);
+    if (!dx && !dw && m && n && k) return ops_fail(ZOA_ERR_ARG, "%s: neither dx nor dw is asked for", me);      // (an empty one may be NULL)
+    if (m && n && k && !work) return ops_fail(ZOA_ERR_ARG, "%s: work is NULL", me);
     void *dyt = static_cast<unsigned char *>(work) + zoa_mx4_size(m, n);
-    zoa_status st = zoa_mx4_quantize(dy, dy_type, m, n, ld_dy, dx ? work : nullptr, dw ? dyt : nullptr, stream);
+    zoa_status st = k ? zoa_mx4_quantize(dy, dy_type, m, n, ld_dy, dx ? work : nullptr, dw ? dyt : nullptr, stream) : ZOA_OK;
     if (st == ZOA_OK && dx && dw && dx_type == dw_type && m && n && k) {
         // Both in one launch where that is no slower: small ones fill the SMs together (rounding and both products, 512 x 1024
         // -> 4096: 25.7 -> 22.7 us, 1777 x 1001 -> 1333 30.8 -> 24.7), of large ones the last tiles of the longer sums run

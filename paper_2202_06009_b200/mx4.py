@@ -26,7 +26,7 @@ def _matrix(x, what):
     rows, cols = x.shape
     ld, step = x.stride()
     if ld < cols or step != 1:
-        if (step != 1 and cols > 1) or (ld < cols and rows > 1):
+        if rows and ((step != 1 and cols > 1) or (ld < cols and rows > 1)):
             raise ValueError(f"the rows of {what} must be contiguous and must not overlap")
         ld = max(ld, cols)
     return code, rows, cols, ld

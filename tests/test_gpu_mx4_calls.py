@@ -66,3 +66,21 @@ def test_gradients_that_autograd_broadcasts(tokens, k, n, dtype):
         loss(y).backward()
         dx, dw = mx4_linear_backward(y.grad.contiguous(), mx4_linear_forward(x, w)[1])
         assert torch.equal(xa.grad, dx) and torch.equal(wa.grad, dw)
+
+
+@pytest.mark.parametrize("need_dx,need_dw", [(True, True), (True, False), (False, True), (False, False)])
+@pytest.mark.parametrize("m,n,k", [(0, 40, 64), (5, 0, 64), (5, 40, 0), (0, 0, 64), (0, 40, 0), (5, 0, 0), (0, 0, 0)])
+def test_empty_training_steps(m, n, k, need_dx, need_dw):
+    """No tokens, no outputs or no inputs: results are empty or, as empty sums, zero."""
+    x, w = torch.ones(m, k, device="cuda"), torch.ones(n, k, device="cuda")
+    y, saved = mx4_linear_forward(x, w)
+    assert y.shape == (m, n) and not y.any()
+    dx, dw = mx4_linear_backward(torch.ones(m, n, device="cuda"), saved, need_dx, need_dw)
+    assert (dx is not None) == need_dx and (dw is not None) == need_dw
+    for got, shape in ((dx, (m, k)), (dw, (n, k))):
+        assert got is None or (got.shape == shape and not got.any())
+    xa, wa = x.clone().requires_grad_(need_dx), w.clone().requires_grad_(need_dw)
+    if need_dx or need_dw:
+        Mx4LinearFunction.apply(xa, wa).sum().backward()
+        assert xa.grad is None or (xa.grad.shape == x.shape and not xa.grad.any())
+        assert wa.grad is None or (wa.grad.shape == w.shape and not wa.grad.any())
