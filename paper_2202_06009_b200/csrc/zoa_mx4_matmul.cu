@@ -1053,9 +1053,10 @@ extern "C" zoa_status zoa_mx4_linear(const void *x, int dtype, size_t m, size_t 
                                      size_t ld, void *work, void *stream)
 {
     const char *me = "zoa_mx4_linear";
+    if (!m || !n) return check_product(me, m, n, k, out, dtype, ld);
     const int rows = few_rows(m, n, k);
-    if (!rows || !m || !n || !k) {
-        if (m && n && k && !work) return ops_fail(ZOA_ERR_ARG, "%s: work is NULL", me);
+    if (!rows || !k) {
+        if (k && !work) return ops_fail(ZOA_ERR_ARG, "%s: work is NULL", me);
         const zoa_status st = zoa_mx4_quantize(x, dtype, m, k, ldx, work, nullptr, stream);
         return st != ZOA_OK ? st : zoa_mx4_matmul(work, b, m, n, k, out, dtype, ld, stream);
     }

@@ -4,7 +4,8 @@ Tolerances are test_gpu_mx4.assert_product's."""
 import pytest
 import torch
 
-from paper_2202_06009_b200 import Mx4LinearFunction, mx4_linear_backward, mx4_linear_forward, mx4_matmul, mx4_quantize
+from paper_2202_06009_b200 import (Mx4LinearFunction, mx4_linear, mx4_linear_backward, mx4_linear_forward, mx4_matmul,
+                                   mx4_quantize)
 from test_gpu_mx4 import ULP, data
 
 pytestmark = pytest.mark.gpu
@@ -84,3 +85,11 @@ def test_empty_training_steps(m, n, k, need_dx, need_dw):
         Mx4LinearFunction.apply(xa, wa).sum().backward()
         assert xa.grad is None or (xa.grad.shape == x.shape and not xa.grad.any())
         assert wa.grad is None or (wa.grad.shape == w.shape and not wa.grad.any())
+
+
+@pytest.mark.parametrize("m", [0, 1, 2, 4, 5, 40])
+@pytest.mark.parametrize("n,k", [(0, 64), (40, 0), (0, 0), (0, 5000)])
+def test_linear_without_outputs_or_inputs(m, n, k):
+    w = mx4_quantize(torch.ones(n, k, device="cuda"))
+    y = mx4_linear(torch.ones(m, k, device="cuda"), w)
+    assert y.shape == (m, n) and not y.any()
