@@ -20,7 +20,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 if ROOT not in sys.path:
     sys.path.insert(0, ROOT)
 
-from paper_2202_06009_b200 import Mx4LinearFunction, Zoa, distill_topk_grad, mx4_linear, mx4_quantize  # noqa: E402
+from paper_2202_06009_b200 import Mx4LinearFunction, Zoa, distill_topk_grad, mx4_linear, mx4_quantize, ops_check_device  # noqa: E402
 
 
 class Student:
@@ -91,6 +91,7 @@ def train(steps=60, workers=4, vocab=2003, hidden=256, layers=2, tokens=512, top
             opt.step_auto(grads, lr, t)
             losses.append(mean)
         opt.check_device()
+        ops_check_device()
         generated = student.generate([p.clone() for p in student.split(opt.device_view("x", 0))], torch.zeros(1, dtype=torch.long, device="cuda"), 8)
     return [float(x) for x in losses], generated
 

@@ -409,11 +409,15 @@ const char *zoa_static_last_error(void);
  * What produces the gradients of a step when the model's linear layers run in 4
  * bits and a stored teacher gives the loss: 4-bit microscaled matrices, their
  * products, and distillation from a teacher's top logits.  No handle: every call
- * works on buffers the caller owns, on the current device, allocates nothing,
+ * works on buffers the caller owns, on the current device, allocates nothing (but,
+ * at the first call on a device, one word of pinned host memory),
  * checks its arguments before anything is enqueued (ZOA_ERR_ARG), enqueues on
  * `stream` and does not synchronise.  A call that fails returns a status; its text
  * is zoa_ops_last_error() of the same thread.  Calls may be made from several
- * threads.  The first call of each kind on a device looks up addresses and raises
+ * threads.  Once a kernel has given up on a bounded wait, every call that enqueues work on
+ * that device returns ZOA_ERR_DEVICE (without synchronising; the news travels through
+ * that word) until zoa_ops_check_device has reported and cleared it.
+ * The first call of each kind on a device allocates that word, looks up addresses and raises
  * kernels' shared-memory limits: make it before any stream capture starts.  (The
  * paper has no counterpart to these entry points.)
  *

@@ -51,7 +51,7 @@ __device__ __forceinline__ unsigned long long timer_ns()
     return t;
 }
 struct WaitLimit {
-    int *error_word;            // set when a wait ran out
+    int *error_word;            // set when a wait ran out: in host memory
     unsigned long long ns;
 };
 // False if the block has given up or the limit ran out (both flags are then set).
@@ -68,7 +68,8 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
             if (start == 0) start = now;
             if (now - start > limit.ns) {
                 *gave_up = 1;
-                atomicExch(limit.error_word, 1);
+                *reinterpret_cast<volatile int *>(limit.error_word) = 1;
+                __threadfence_system();
                 return false;
             }
         }

@@ -606,6 +606,7 @@ void launch_kernel(const DistillArgs &a, int blocks, const WaitLimit &wait_limit
 zoa_status launch(const char *me, const zoa_distill_args *x, const float *stats_in, const float *grad_loss, float *loss, float *stats,
                   void *grad, size_t ld_grad, void *stream)
 {
+    if (ops_gave_up()) return ops_refuse(me);
     if (!x) return ops_fail(ZOA_ERR_ARG, "%s: args is NULL", me);
     if (!dtype_ok(x->dtype)) return ops_fail(ZOA_ERR_ARG, "%s: unknown element type %d", me, x->dtype);
     if (x->vocab < 1 || x->vocab > kMaxVocab) return ops_fail(ZOA_ERR_ARG, "%s: vocab must be in [1, 2^20]", me);

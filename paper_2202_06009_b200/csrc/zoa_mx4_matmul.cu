@@ -1015,6 +1015,7 @@ extern "C" zoa_status zoa_mx4_matmul(const void *a, const void *b, size_t m, siz
                                      void *stream)
 {
     const char *me = "zoa_mx4_matmul";
+    if (ops_gave_up()) return ops_refuse(me);
     zoa_status st = check_product(me, m, n, k, out, dtype, ld);
     if (st != ZOA_OK || m == 0 || n == 0) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -1053,6 +1054,7 @@ extern "C" zoa_status zoa_mx4_linear(const void *x, int dtype, size_t m, size_t 
                                      size_t ld, void *work, void *stream)
 {
     const char *me = "zoa_mx4_linear";
+    if (ops_gave_up()) return ops_refuse(me);
     if (!m || !n) return check_product(me, m, n, k, out, dtype, ld);
     const int rows = few_rows(m, n, k);
     if (!rows || !k) {
@@ -1092,6 +1094,7 @@ extern "C" zoa_status zoa_mx4_linear_forward(const void *x, int x_type, size_t l
                                              size_t n, size_t k, void *y, size_t ldy, void *xt, void *wt, void *work, void *stream)
 {
     const char *me = "zoa_mx4_linear_forward";
+    if (ops_gave_up()) return ops_refuse(me);
     if (m && n && k && (!xt || !wt || !work)) return ops_fail(ZOA_ERR_ARG, "%s: a NULL pointer", me);
     void *wq = static_cast<unsigned char *>(work) + zoa_mx4_size(m, k);
     zoa_status st = mx4_check_source(me, x, x_type, m, k, ldx, work, xt);
@@ -1112,6 +1115,7 @@ extern "C" zoa_status zoa_mx4_linear_backward(const void *dy, int dy_type, size_
                                               void *work, void *stream)
 {
     const char *me = "zoa_mx4_linear_backward";
+    if (ops_gave_up()) return ops_refuse(me);
     if (!dx && !dw && m && n && k) return ops_fail(ZOA_ERR_ARG, "%s: neither dx nor dw is asked for", me);      // (an empty one may be NULL)
     if (m && n && k && !work) return ops_fail(ZOA_ERR_ARG, "%s: work is NULL", me);
     void *dyt = static_cast<unsigned char *>(work) + zoa_mx4_size(m, n);

@@ -410,6 +410,7 @@ extern "C" zoa_status zoa_mx4_quantize(const void *x, int dtype, size_t rows, si
                                        void *stream)
 {
     const char *me = "zoa_mx4_quantize";
+    if (ops_gave_up()) return ops_refuse(me);
     const zoa_status st = mx4_check_source(me, x, dtype, rows, cols, ld, out, out_t);
     if (st != ZOA_OK || rows == 0 || cols == 0) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -430,6 +431,7 @@ extern "C" zoa_status zoa_mx4_quantize(const void *x, int dtype, size_t rows, si
 extern "C" zoa_status zoa_mx4_dequantize(const void *q, size_t rows, size_t cols, void *out, int dtype, size_t ld, void *stream)
 {
     const char *me = "zoa_mx4_dequantize";
+    if (ops_gave_up()) return ops_refuse(me);
     if (!dtype_ok(dtype)) return ops_fail(ZOA_ERR_ARG, "%s: unknown element type %d", me, dtype);
     if (rows > kMxMaxSide || cols > kMxMaxSide) return ops_fail(ZOA_ERR_ARG, "%s: rows and cols must be at most 2^30", me);
     if (rows == 0 || cols == 0) return ZOA_OK;

@@ -4,14 +4,13 @@
 #include <atomic>
 #include <cstdarg>
 #include <cstdio>
-#include <mutex>
+#include <new>
 
 namespace zoa {
 
 static thread_local char t_error[320] = "";
 static std::atomic<int> g_wait_limit_ms{2000};
 static std::atomic<int> g_test_stop{0};
-static __device__ int g_ops_error = 0;
 
 zoa_status ops_fail(zoa_status s, const char *fmt, ...)
 {
@@ -39,19 +38,51 @@ int ops_sm_count()
     return n;
 }
 
+// A word of pinned, mapped host memory for each device, made once and kept: kernels set it, the host reads it without
+// synchronising.
+struct ErrorWord {
+    volatile int *host;
+    int *device;
+};
+static std::atomic<ErrorWord *> g_words[64];
+static std::atomic<ErrorWord *> *word_of_device()
+{
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64 ? &g_words[dev] : nullptr;
+}
+
 int *ops_error_word()
 {
-    static std::atomic<int *> word[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-    int *p = word[dev].load(std::memory_order_acquire);
-    if (!p) {
-        void *q = nullptr;
-        if (cudaGetSymbolAddress(&q, g_ops_error) != cudaSuccess) return nullptr;
-        p = static_cast<int *>(q);
-        word[dev].store(p, std::memory_order_release);
+    std::atomic<ErrorWord *> *at = word_of_device();
+    if (!at) return nullptr;
+    ErrorWord *word = at->load(std::memory_order_acquire);
+    if (word) return word->device;
+    void *host = nullptr, *device = nullptr;
+    word = new (std::nothrow) ErrorWord;
+    if (!word || cudaHostAlloc(&host, sizeof(int), cudaHostAllocMapped | cudaHostAllocPortable) != cudaSuccess ||
+        cudaHostGetDevicePointer(&device, host, 0) != cudaSuccess) {
+        if (host) cudaFreeHost(host);
+        delete word;
+        return nullptr;
     }
-    return p;
+    *word = ErrorWord{static_cast<int *>(host), static_cast<int *>(device)};
+    *word->host = 0;
+    ErrorWord *other = nullptr;
+    if (at->compare_exchange_strong(other, word, std::memory_order_acq_rel)) return word->device;
+    cudaFreeHost(host);          // another thread was first
+    delete word;
+    return other->device;
+}
+
+bool ops_gave_up()
+{
+    const std::atomic<ErrorWord *> *at = word_of_device();
+    const ErrorWord *word = at ? at->load(std::memory_order_acquire) : nullptr;
+    return word && *word->host != 0;
+}
+zoa_status ops_refuse(const char *what)
+{
+    return ops_fail(ZOA_ERR_DEVICE, "%s: an earlier kernel gave up on a bounded wait; its result is undefined (zoa_ops_check_device clears this)", what);
 }
 
 unsigned long long ops_wait_limit_ns() { return 1000000ull * (unsigned long long)g_wait_limit_ms.load(); }
@@ -78,14 +109,9 @@ extern "C" zoa_status zoa_ops_set_option(int option, int value)
 
 extern "C" zoa_status zoa_ops_check_device(void)
 {
-    int *word = ops_error_word();
-    cudaError_t e = cudaDeviceSynchronize();
-    int set = 0;
-    if (e == cudaSuccess && word) e = cudaMemcpy(&set, word, sizeof set, cudaMemcpyDeviceToHost);
-    if (e != cudaSuccess || !word) return ops_fail(ZOA_ERR_CUDA, "zoa_ops_check_device: %s", cudaGetErrorString(e));
-    if (!set) return ZOA_OK;
-    set = 0;
-    e = cudaMemcpy(word, &set, sizeof set, cudaMemcpyHostToDevice);
+    const cudaError_t e = cudaDeviceSynchronize();
     if (e != cudaSuccess) return ops_fail(ZOA_ERR_CUDA, "zoa_ops_check_device: %s", cudaGetErrorString(e));
+    if (!ops_gave_up()) return ZOA_OK;
+    *word_of_device()->load(std::memory_order_acquire)->host = 0;
     return ops_fail(ZOA_ERR_DEVICE, "a kernel gave up on a bounded wait; its result is undefined");
 }

@@ -20,8 +20,11 @@ zoa_status ops_fail(zoa_status s, const char *fmt, ...) __attribute__((format(pr
 zoa_status ops_launched(const char *what);
 // SMs of the current device (cached); 0 if the device cannot be asked.
 int ops_sm_count();
-// This device's word that a kernel sets when a bounded wait ran out; NULL if it cannot be had.
+// The device's address of the current device's word that a kernel sets when a bounded wait ran out; NULL if it cannot be had.
 int *ops_error_word();
+// Whether a kernel has set it since zoa_ops_check_device last cleared it: every call that enqueues then returns ops_refuse.
+bool ops_gave_up();
+zoa_status ops_refuse(const char *what);
 // ZOA_OPT_WAIT_LIMIT_MS in nanoseconds and ZOA_OPT_TEST_STOP_AFTER_TILES, as zoa_ops_set_option last left them.
 unsigned long long ops_wait_limit_ns();
 int ops_test_stop();

@@ -4,8 +4,10 @@ Tolerances are test_gpu_mx4.assert_product's."""
 import pytest
 import torch
 
-from paper_2202_06009_b200 import (Mx4LinearFunction, mx4_linear, mx4_linear_backward, mx4_linear_forward, mx4_matmul,
-                                   mx4_quantize)
+from paper_2202_06009_b200 import (Mx4LinearFunction, ZoaError, binding as B, distill_topk, distill_topk_grad, mx4_linear,
+                                   mx4_linear_backward, mx4_linear_forward, mx4_matmul, mx4_quantize, mx4_quantize_both,
+                                   ops_check_device)
+from test_gpu_distill import problem
 from test_gpu_mx4 import ULP, data
 
 pytestmark = pytest.mark.gpu
@@ -93,3 +95,30 @@ def test_linear_without_outputs_or_inputs(m, n, k):
     w = mx4_quantize(torch.ones(n, k, device="cuda"))
     y = mx4_linear(torch.ones(m, k, device="cuda"), w)
     assert y.shape == (m, n) and not y.any()
+
+
+def test_a_kernel_that_gave_up_is_reported_by_the_next_call():
+    """Without a synchronising check: every operator refuses until zoa_ops_check_device has reported it."""
+    x, w = data(200, 4096, torch.bfloat16, 1), data(200, 4096, torch.bfloat16, 2)
+    a, b = mx4_quantize(x), mx4_quantize(w)
+    want = mx4_matmul(a, b)
+    p = problem(4, 60, 6, torch.float32, 2)
+    B.zoa_ops_check_device()
+    try:
+        B.zoa_ops_set_option(B.OPT_WAIT_LIMIT_MS, 20)
+        B.zoa_ops_set_option(B.OPT_TEST_STOP_AFTER_TILES, 2)
+        mx4_matmul(a, b)
+    finally:
+        B.zoa_ops_set_option(B.OPT_WAIT_LIMIT_MS, 2000)
+        B.zoa_ops_set_option(B.OPT_TEST_STOP_AFTER_TILES, 0)
+    torch.cuda.synchronize()
+    for call in (lambda: mx4_matmul(a, b), lambda: mx4_quantize(x), lambda: a.dequantize(), lambda: mx4_linear(x, b), lambda: mx4_linear(x[:1], b),
+                 lambda: mx4_linear_forward(x, w), lambda: mx4_quantize_both(x), lambda: distill_topk(**p), lambda: distill_topk_grad(**p)):
+        with pytest.raises(ZoaError) as e:
+            call()
+        assert e.value.status == B.ERR_DEVICE
+    with pytest.raises(ZoaError) as e:
+        ops_check_device()
+    assert e.value.status == B.ERR_DEVICE
+    ops_check_device()
+    assert torch.equal(mx4_matmul(a, b), want)
