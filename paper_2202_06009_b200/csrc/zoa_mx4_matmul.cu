@@ -1058,8 +1058,10 @@ extern "C" zoa_status zoa_mx4_linear(const void *x, int dtype, size_t m, size_t 
     if (!m || !n) return check_product(me, m, n, k, out, dtype, ld);
     const int rows = few_rows(m, n, k);
     if (!rows || !k) {
-        if (k && !work) return ops_fail(ZOA_ERR_ARG, "%s: work is NULL", me);
-        const zoa_status st = zoa_mx4_quantize(x, dtype, m, k, ldx, work, nullptr, stream);
+        zoa_status st = mx4_check_source(me, x, dtype, m, k, ldx, work, nullptr);
+        if (st == ZOA_OK) st = check_product(me, m, n, k, out, dtype, ld);
+        if (st == ZOA_OK && k) st = check_matrix(me, "b", b);
+        if (st == ZOA_OK) st = zoa_mx4_quantize(x, dtype, m, k, ldx, work, nullptr, stream);
         return st != ZOA_OK ? st : zoa_mx4_matmul(work, b, m, n, k, out, dtype, ld, stream);
     }
     if (!dtype_ok(dtype)) return ops_fail(ZOA_ERR_ARG, "%s: unknown element type %d", me, dtype);
@@ -1099,6 +1101,7 @@ extern "C" zoa_status zoa_mx4_linear_forward(const void *x, int x_type, size_t l
     void *wq = static_cast<unsigned char *>(work) + zoa_mx4_size(m, k);
     zoa_status st = mx4_check_source(me, x, x_type, m, k, ldx, work, xt);
     if (st == ZOA_OK) st = mx4_check_source(me, w, w_type, n, k, ldw, wq, wt);
+    if (st == ZOA_OK) st = check_product(me, m, n, k, y, x_type, ldy);
     if (st != ZOA_OK) return st;
     if (x_type == w_type && m && n && k) {      // one launch for both
         st = mx4_launch_both(me, x_type, mx4_both_job(x, x_type, m, k, ldx, work, xt), mx4_both_job(w, w_type, n, k, ldw, wq, wt),
@@ -1119,16 +1122,20 @@ extern "C" zoa_status zoa_mx4_linear_backward(const void *dy, int dy_type, size_
     if (!dx && !dw && m && n && k) return ops_fail(ZOA_ERR_ARG, "%s: neither dx nor dw is asked for", me);      // (an empty one may be NULL)
     if (m && n && k && !work) return ops_fail(ZOA_ERR_ARG, "%s: work is NULL", me);
     void *dyt = static_cast<unsigned char *>(work) + zoa_mx4_size(m, n);
-    zoa_status st = k ? zoa_mx4_quantize(dy, dy_type, m, n, ld_dy, dx ? work : nullptr, dw ? dyt : nullptr, stream) : ZOA_OK;
+    void *dy_rows = dx ? work : nullptr, *dy_columns = dw ? dyt : nullptr;
+    zoa_status st = k ? mx4_check_source(me, dy, dy_type, m, n, ld_dy, dy_rows, dy_columns) : ZOA_OK;
+    if (st == ZOA_OK && dx) st = check_product(me, m, k, n, dx, dx_type, ld_dx);
+    if (st == ZOA_OK && dw) st = check_product(me, n, k, m, dw, dw_type, ld_dw);
+    if (st == ZOA_OK && dx && m && n && k) st = check_matrix(me, "wt", wt);
+    if (st == ZOA_OK && dw && m && n && k) st = check_matrix(me, "xt", xt);
+    if (st == ZOA_OK && k) st = zoa_mx4_quantize(dy, dy_type, m, n, ld_dy, dy_rows, dy_columns, stream);
     if (st == ZOA_OK && dx && dw && dx_type == dw_type && m && n && k) {
         // Both in one launch where that is no slower: small ones fill the SMs together (rounding and both products, 512 x 1024
         // -> 4096: 25.7 -> 22.7 us, 1777 x 1001 -> 1333 30.8 -> 24.7), of large ones the last tiles of the longer sums run
         // beside the others' (16384 x 1600 -> 6400: 237 -> 217).
         MatmulArgs of_x{}, of_w{};
         int sms = 0;
-        st = check_product(me, m, k, n, dx, dx_type, ld_dx);
-        if (st == ZOA_OK) st = check_product(me, n, k, m, dw, dw_type, ld_dw);
-        if (st == ZOA_OK) st = product_args(me, work, wt, m, k, n, dx, dx_type, ld_dx, of_x, sms);
+        st = product_args(me, work, wt, m, k, n, dx, dx_type, ld_dx, of_x, sms);
         if (st == ZOA_OK) st = product_args(me, dyt, xt, n, k, m, dw, dw_type, ld_dw, of_w, sms);
         if (st != ZOA_OK) return st;
         double together = 0.0;

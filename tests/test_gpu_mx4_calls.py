@@ -122,3 +122,52 @@ def test_a_kernel_that_gave_up_is_reported_by_the_next_call():
     assert e.value.status == B.ERR_DEVICE
     ops_check_device()
     assert torch.equal(mx4_matmul(a, b), want)
+
+
+def test_composed_calls_check_everything_first():
+    """A call that is refused has enqueued nothing: neither its work area nor a result is written."""
+    m, n, k = 40, 48, 64
+    x, w, dy = data(m, k, torch.float32, 1), data(n, k, torch.float32, 2), data(m, n, torch.float32, 3)
+    wq = mx4_quantize(w)
+    room = lambda *sizes: [torch.full((s,), 7, dtype=torch.uint8, device="cuda") for s in sizes]  # noqa: E731
+    size = B.zoa_mx4_size
+    xt, wt, work = room(size(k, m), size(k, n), 8 * size(128, 256))
+    y, dx, dw = torch.full((m, n), 7.0, device="cuda"), torch.full((m, k), 7.0, device="cuda"), torch.full((n, k), 7.0, device="cuda")
+    p = {name: t.data_ptr() for name, t in (("x", x), ("w", w), ("dy", dy), ("xt", xt), ("wt", wt), ("work", work), ("y", y), ("dx", dx),
+                                            ("dw", dw), ("wq", wq.data))}
+
+    def linear(x=p["x"], dtype=0, ldx=k, b=p["wq"], out=p["y"], ld=n, work=p["work"]):
+        B.zoa_mx4_linear(x, dtype, m, k, ldx, b, n, out, ld, work)
+
+    def forward(x=p["x"], x_type=0, ldx=k, w=p["w"], w_type=0, ldw=k, y=p["y"], ldy=n, xt=p["xt"], wt=p["wt"], work=p["work"]):
+        B.zoa_mx4_linear_forward(x, x_type, ldx, w, w_type, ldw, m, n, k, y, ldy, xt, wt, work)
+
+    def backward(dy=p["dy"], dy_type=0, ld_dy=n, xt=p["xt"], wt=p["wt"], dx=p["dx"], dx_type=0, ld_dx=k, dw=p["dw"], dw_type=0, ld_dw=k,
+                 work=p["work"]):
+        B.zoa_mx4_linear_backward(dy, dy_type, ld_dy, m, n, k, xt, wt, dx, dx_type, ld_dx, dw, dw_type, ld_dw, work)
+
+    def few(b=p["wq"], out=p["y"], ld=n, ldx=k, x=p["x"]):       # rounded inside the product
+        B.zoa_mx4_linear(x, 0, 2, k, ldx, b, n, out, ld, None)
+
+    bad = [(linear, dict(x=None)), (linear, dict(dtype=3)), (linear, dict(ldx=k - 1)), (linear, dict(b=None)), (linear, dict(b=p["wq"] + 8)),
+           (linear, dict(out=None)), (linear, dict(ld=n - 1)), (linear, dict(out=p["y"] + 2)), (linear, dict(work=None)), (linear, dict(work=p["work"] + 8)),
+           (few, dict(b=None)), (few, dict(out=None)), (few, dict(ld=n - 1)), (few, dict(ldx=k - 1)), (few, dict(x=None)),
+           (forward, dict(x=None)), (forward, dict(w=None)), (forward, dict(y=None)), (forward, dict(ldy=n - 1)), (forward, dict(y=p["y"] + 2)),
+           (forward, dict(xt=None)), (forward, dict(wt=None)), (forward, dict(work=None)), (forward, dict(xt=p["xt"] + 4)), (forward, dict(wt=p["wt"] + 4)),
+           (forward, dict(work=p["work"] + 4)), (forward, dict(w_type=9)), (forward, dict(x_type=9)), (forward, dict(ldw=k - 1)), (forward, dict(ldx=k - 1)),
+           (backward, dict(dy=None)), (backward, dict(dy_type=9)), (backward, dict(ld_dy=n - 1)), (backward, dict(xt=None)), (backward, dict(wt=None)),
+           (backward, dict(xt=p["xt"] + 4)), (backward, dict(wt=p["wt"] + 4)), (backward, dict(dx_type=9)), (backward, dict(dw_type=9)),
+           (backward, dict(ld_dx=k - 1)), (backward, dict(ld_dw=k - 1)), (backward, dict(dx=p["dx"] + 2)), (backward, dict(dw=p["dw"] + 2)),
+           (backward, dict(dx=None, dw=None)), (backward, dict(work=None)), (backward, dict(work=p["work"] + 8)),
+           (backward, dict(dx=None, ld_dw=k - 1)), (backward, dict(dw=None, ld_dx=k - 1)), (backward, dict(dw=None, wt=None)),
+           (backward, dict(dx=None, xt=None)), (backward, dict(dw_type=1, dw=p["dw"] + 1)), (backward, dict(dw_type=1, ld_dw=k - 1))]
+    written = []
+    for call, change in bad:
+        with pytest.raises(ZoaError) as e:
+            call(**change)
+        assert e.value.status == B.ERR_ARG, (call.__name__, change, str(e.value))
+        if not all((t == 7).all() for t in (xt, wt, work, y, dx, dw)):
+            written.append((call.__name__, list(change)))
+            for t in (xt, wt, work, y, dx, dw):
+                t.fill_(7)
+    assert not written
