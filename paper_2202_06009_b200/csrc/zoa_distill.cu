@@ -622,6 +622,9 @@ zoa_status launch(const char *me, const zoa_distill_args *x, const float *stats_
     const size_t e = dtype_bytes(x->dtype);
     if (reinterpret_cast<uintptr_t>(x->logits) % e || reinterpret_cast<uintptr_t>(x->teacher) % e || reinterpret_cast<uintptr_t>(grad) % e)
         return ops_fail(ZOA_ERR_ARG, "%s: a matrix is not aligned to its element type", me);
+    const uintptr_t words = reinterpret_cast<uintptr_t>(x->index) | reinterpret_cast<uintptr_t>(x->teacher_lse) | reinterpret_cast<uintptr_t>(x->labels) |
+                            reinterpret_cast<uintptr_t>(x->row_weight) | reinterpret_cast<uintptr_t>(loss) | reinterpret_cast<uintptr_t>(grad_loss);
+    if (words % 4) return ops_fail(ZOA_ERR_ARG, "%s: a vector or the list is not 4-byte aligned", me);
     if (!aligned16(stats) || !aligned16(stats_in)) return ops_fail(ZOA_ERR_ARG, "%s: stats must be 16-byte aligned", me);
     if (grad == x->logits && ld_grad != x->ld_logits)
         return ops_fail(ZOA_ERR_ARG, "%s: a gradient that replaces the logits has their ld", me);

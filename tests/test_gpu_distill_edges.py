@@ -104,3 +104,24 @@ def test_temperatures_whose_reciprocal_overflows_are_refused():
         assert e.value.status == B.ERR_ARG
     loss = distill_topk(**dict(p, temperature=1e-30))
     assert not torch.isnan(loss).any()
+
+
+def test_pointers_that_are_not_aligned_are_refused():
+    p = problem(4, 50, 6, torch.float32, 1, tail=True, labels=True)
+    loss, stats = distill_topk(**p, stats=True)
+    grad, ones = torch.empty(4, 50, device="cuda"), torch.ones(4, device="cuda")
+    fields = dict(logits=p["logits"].data_ptr(), index=p["index"].data_ptr(), teacher=p["teacher"].data_ptr(), teacher_lse=p["teacher_lse"].data_ptr(),
+                  labels=p["labels"].data_ptr(), row_weight=p["row_weight"].data_ptr(), rows=4, vocab=50, top=6, ld_logits=50, dtype=B.F32,
+                  temperature=1.0, soft_weight=1.0, hard_weight=0.0)
+    calls = []
+    for name in ("logits", "index", "teacher", "teacher_lse", "labels", "row_weight"):
+        args = B.DistillArgs(**dict(fields, **{name: fields[name] + 2}))
+        calls.append(lambda args=args: B.zoa_distill_topk(args, loss.data_ptr(), None, None, 0))
+    good = B.DistillArgs(**fields)
+    calls += [lambda: B.zoa_distill_topk(good, loss.data_ptr() + 2, None, None, 0), lambda: B.zoa_distill_topk(good, None, stats.data_ptr() + 4, None, 0),
+              lambda: B.zoa_distill_topk(good, None, None, grad.data_ptr() + 2, 50),
+              lambda: B.zoa_distill_topk_backward(good, stats.data_ptr(), ones.data_ptr() + 1, grad.data_ptr(), 50)]
+    for call in calls:
+        with pytest.raises(ZoaError) as e:
+            call()
+        assert e.value.status == B.ERR_ARG
