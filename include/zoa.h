@@ -491,13 +491,15 @@ zoa_status zoa_mx4_linear_backward(const void *dy, int dy_type, size_t ld_dy, si
  *   grad = d loss / d z
  * index: int32 [rows, top]; an entry outside [0, vocab) is skipped (shorter lists end
  * in -1), a token listed twice counts with both probabilities, a row with no entry
- * left, or none above -inf, has no soft part.  A term with p = 0 is 0.
+ * left (or, where teacher_lse is NULL, none above -inf) has no soft part.  A term with
+ * p = 0 is 0.
  * labels (may be NULL): int32 [rows]; a row whose label is outside [0, vocab) has
  * no hard part.  A row of weight 0 gives loss 0 and gradient 0 whatever it holds.
- * Logits of -inf are tokens masked out (q = 0, gradient 0); a row of nothing else
- * gives loss 0 and gradient 0.  The p_r term is left out of a row whose q_r is 0 or
- * below 1e-30.  A NaN or +inf logit makes its row NaN, and so
- * does a NaN among the listed teacher's logits.  All sums in binary32; the
+ * Logits of -inf are tokens masked out: q = 0, and gradient 0 unless the token is the
+ * label or listed with p > 0 (the loss is then infinite); a row of nothing else
+ * gives loss 0 and gradient 0.  The p_r term is left out, of the loss and so of the
+ * gradient, in a row whose q_r is 0 or below 1e-30.  A NaN or +inf logit makes its row
+ * NaN, and so does a NaN among the teacher's listed logits.  All sums in binary32; the
  * order of a row's sums depends on the sizes of the call, the alignment of its
  * rows and the outputs asked for (a loss alone and one beside a gradient may differ
  * in their last bits): equal calls give equal bits.  Limits: vocab in
