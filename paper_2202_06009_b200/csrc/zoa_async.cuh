@@ -1,4 +1,4 @@
-// Barriers and bulk copies of the handle-free operators' kernels; every wait is bounded.
+// Barriers of the handle-free operators' kernels; every wait is bounded.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -16,10 +16,6 @@ __device__ __forceinline__ void mbar_init_done() { asm volatile("fence.mbarrier_
 __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 // kCluster: what arrives on the barrier are other blocks of the cluster, with data of theirs.
 template <bool kCluster = false>
@@ -102,20 +98,6 @@ __device__ __forceinline__ void store_there(uint32_t addr, uint32_t rank, int v)
 {
     asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(address_at(addr, rank)), "r"(v) : "memory");
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
-}
-__device__ __forceinline__ void bulk_store(void *dst, uint32_t src, uint32_t bytes)
-{
-    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-__device__ __forceinline__ void bulk_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-__device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ uint32_t cluster_rank()
 {
     uint32_t r;

@@ -53,11 +53,9 @@ __device__ __forceinline__ void mma_mx4(uint32_t one, uint32_t d, uint64_t a, ui
 }
 // 32 rows x 16 bytes of scales to four columns of tensor memory, repeated for the four groups of 32 lanes.
 #define ZOA_IF_ONE(instruction) "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %0, 0;\n\t@q " instruction "\n\t}"
-template <bool kPair = false>
 __device__ __forceinline__ void copy_scales(uint32_t one, uint32_t tmem, uint64_t desc)
 {
-    if constexpr (kPair) asm volatile(ZOA_IF_ONE("tcgen05.cp.cta_group::2.32x128b.warpx4 [%1], %2;") ::"r"(one), "r"(tmem), "l"(desc) : "memory");
-    else asm volatile(ZOA_IF_ONE("tcgen05.cp.cta_group::1.32x128b.warpx4 [%1], %2;") ::"r"(one), "r"(tmem), "l"(desc) : "memory");
+    asm volatile(ZOA_IF_ONE("tcgen05.cp.cta_group::1.32x128b.warpx4 [%1], %2;") ::"r"(one), "r"(tmem), "l"(desc) : "memory");
 }
 // The work issued so far arrives on the barrier when it is done; of a pair, at the same place in both blocks.
 __device__ __forceinline__ void commit(uint32_t one, uint32_t bar)

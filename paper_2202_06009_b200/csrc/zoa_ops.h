@@ -92,17 +92,10 @@ template <> __device__ __forceinline__ void unpack2<__nv_bfloat16>(uint32_t w, f
     hi = __uint_as_float(w & 0xFFFF0000u);
 }
 
-// A 16-byte vector of T (8 or 4 elements) to and from binary32.
+// A 16-byte vector of T (8 or 4 elements) from binary32.
 template <typename T>
 struct Vec {
     static constexpr int kElems = 16 / (int)sizeof(T);
-    static __device__ __forceinline__ void unpack(const uint4 &w, float *v)
-    {
-        unpack2<T>(w.x, v[0], v[1]);
-        unpack2<T>(w.y, v[2], v[3]);
-        unpack2<T>(w.z, v[4], v[5]);
-        unpack2<T>(w.w, v[6], v[7]);
-    }
     static __device__ __forceinline__ uint4 pack(const float *v)
     {
         return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
@@ -111,13 +104,6 @@ struct Vec {
 template <>
 struct Vec<float> {
     static constexpr int kElems = 4;
-    static __device__ __forceinline__ void unpack(const uint4 &w, float *v)
-    {
-        v[0] = __uint_as_float(w.x);
-        v[1] = __uint_as_float(w.y);
-        v[2] = __uint_as_float(w.z);
-        v[3] = __uint_as_float(w.w);
-    }
     static __device__ __forceinline__ uint4 pack(const float *v)
     {
         return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
