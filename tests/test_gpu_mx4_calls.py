@@ -1,14 +1,16 @@
 """The 4-bit layer's calls in the forms and at the sizes where they can go wrong: rests of the large product's tiles, operands that
 change under repeated calls, gradients that autograd makes, empty sizes, mixed types, one-sided gradients, refusals.
 Tolerances are test_gpu_mx4.assert_product's."""
+import numpy as np
 import pytest
 import torch
 
-from paper_2202_06009_b200 import (Mx4LinearFunction, ZoaError, binding as B, distill_topk, distill_topk_grad, mx4_linear,
+from paper_2202_06009_b200 import (Mx4, Mx4LinearFunction, ZoaError, binding as B, distill_topk, distill_topk_grad, mx4_linear,
                                    mx4_linear_backward, mx4_linear_forward, mx4_matmul, mx4_quantize, mx4_quantize_both,
                                    ops_check_device)
+from plain_ops import round_mx4
 from test_gpu_distill import problem
-from test_gpu_mx4 import ULP, data
+from test_gpu_mx4 import ULP, as64, assert_product, data
 
 pytestmark = pytest.mark.gpu
 
@@ -171,3 +173,45 @@ def test_composed_calls_check_everything_first():
             for t in (xt, wt, work, y, dx, dw):
                 t.fill_(7)
     assert not written
+
+
+@pytest.mark.parametrize("x_type,w_type", [(torch.bfloat16, torch.float32), (torch.float32, torch.bfloat16), (torch.float16, torch.float32),
+                                           (torch.bfloat16, torch.float16)])
+@pytest.mark.parametrize("tokens,k,n", [(1, 33, 40), (50, 100, 70), (300, 256, 513), (1029, 1001, 1333)])
+def test_training_step_of_two_types(tokens, k, n, x_type, w_type):
+    """Activations in 16 bits beside the optimizer's 32-bit weights, as in training, and the other way round."""
+    x, w, dy = data(tokens, k, x_type, 1, 0.5), data(n, k, w_type, 2, 0.1, 0.05), data(tokens, n, x_type, 3, 0.5, 0.01)
+    y, saved = mx4_linear_forward(x, w)
+    dx, dw = mx4_linear_backward(dy, saved)
+    assert y.dtype == dx.dtype == x_type and dw.dtype == w_type
+    x64, w64, dy64 = as64(x), as64(w), as64(dy)
+    assert_product(y, round_mx4(x64), round_mx4(w64), x_type)
+    assert_product(dx, round_mx4(dy64), round_mx4(w64.T), x_type)
+    assert_product(dw, round_mx4(dy64.T), round_mx4(x64.T), w_type)
+    # a gradient of another type than the result's
+    dx2, dw2 = mx4_linear_backward(dy.float(), saved)
+    assert torch.equal(dx, dx2) and torch.equal(dw, dw2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,k,n", [(50, 100, 70), (600, 1500, 2100)])
+def test_one_gradient_alone(tokens, k, n, dtype):
+    x, w, dy = data(tokens, k, dtype, 1, 0.5), data(n, k, dtype, 2, 0.1, 0.05), data(tokens, n, dtype, 3, 0.5, 0.01)
+    saved = mx4_linear_forward(x, w)[1]
+    dx, none = mx4_linear_backward(dy, saved, need_dw=False)
+    assert none is None
+    none, dw = mx4_linear_backward(dy, saved, need_dx=False)
+    assert none is None
+    assert_product(dx, round_mx4(as64(dy)), round_mx4(as64(w).T), dtype)
+    assert_product(dw, round_mx4(as64(dy).T), round_mx4(as64(x).T), dtype)
+    assert mx4_linear_backward(dy, saved, need_dx=False, need_dw=False) == (None, None)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (5, 256), (129, 511), (300, 640), (257, 129)])
+def test_rounding_of_the_transpose_alone(rows, cols, dtype):
+    x = data(rows, cols, dtype, rows + cols, spread=2.0)
+    out_t = Mx4(cols, rows)
+    B.zoa_mx4_quantize(x.data_ptr(), {torch.float32: B.F32, torch.float16: B.F16, torch.bfloat16: B.BF16}[dtype], rows, cols, cols, None,
+                       out_t.data.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert np.array_equal(as64(out_t.dequantize(torch.float32)), round_mx4(as64(x).T))
