@@ -77,26 +77,23 @@ __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, const 
     const unsigned long long start = timer_ns();
     while (!mbar_try(bar, parity) && timer_ns() - start < limit.ns) {}
 }
-// The same place in the shared memory of block `rank` of this cluster.
-__device__ __forceinline__ uint32_t address_at(uint32_t addr, uint32_t rank)
-{
-    uint32_t remote;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
-    return remote;
-}
 // Arrives on the barrier at the same place in block `rank` of this cluster.
 __device__ __forceinline__ void mbar_arrive_at(uint32_t bar, uint32_t rank)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(address_at(bar, rank)) : "memory");
+    uint32_t remote;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(bar), "r"(rank));
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
 }
-// The same without ordering any of this thread's earlier accesses to memory: for tensor memory alone, whose own fences order it.
+// Orders this thread's earlier accesses to its block's shared memory, and what it has seen of others', ahead of its later
+// arrivals at cluster scope.  A release at that scope orders all memory and waits for what is on its way there: 1700 cycles in
+// the pair product.
+__device__ __forceinline__ void release_shared() { asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory"); }
+// Arrives there without ordering earlier accesses: for tensor memory, whose own fences order it, or after release_shared.
 __device__ __forceinline__ void mbar_tell(uint32_t bar, uint32_t rank)
 {
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(address_at(bar, rank)) : "memory");
-}
-__device__ __forceinline__ void store_there(uint32_t addr, uint32_t rank, int v)
-{
-    asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(address_at(addr, rank)), "r"(v) : "memory");
+    uint32_t remote;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(bar), "r"(rank));
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
 }
 __device__ __forceinline__ uint32_t cluster_rank()
 {

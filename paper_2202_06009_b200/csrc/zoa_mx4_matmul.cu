@@ -5,8 +5,6 @@
 
 #include <algorithm>
 
-#include <cuda.h>
-
 namespace zoa {
 namespace {
 
@@ -77,19 +75,6 @@ __device__ __forceinline__ void bulk_load_one(uint32_t one, uint32_t dst, const 
     asm volatile(ZOA_IF_ONE("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%1], [%2], %3, [%4];") ::"r"(one), "r"(dst),
                  "l"(src), "r"(bytes), "r"(bar)
                  : "memory");
-}
-// 128 lines of codes of one tile (see code_lines) to this block's shared memory; their bytes arrive on a barrier of either
-// block of the pair.
-__device__ __forceinline__ void load_lines_one(uint32_t one, uint32_t dst, const CUtensorMap *map, int line, int tile, uint32_t bar)
-{
-    asm volatile(ZOA_IF_ONE("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
-                            "[%1], [%2, {%3, %4, %5}], [%6];") ::"r"(one), "r"(dst), "l"(map), "r"(0), "r"(line), "r"(tile), "r"(bar)
-                 : "memory");
-}
-// Expects `bytes` on a barrier of another block (by mapa).  It orders nothing: what arrives there brings its own order.
-__device__ __forceinline__ void expect_there_one(uint32_t one, uint32_t bar, uint32_t bytes)
-{
-    asm volatile(ZOA_IF_ONE("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%1], %2;") ::"r"(one), "r"(bar), "r"(bytes) : "memory");
 }
 // A bounded wait of a whole warp.
 template <bool kCluster = false>
@@ -314,10 +299,10 @@ __global__ void __launch_bounds__(192) matmul_kernel(const MatmulArgs g, const i
 
 // ---- pairs of SMs, large products --------------------------------------------------------------------------
 // A cluster of two blocks computes 256 x 256 of C at a time, each block the sums of 128 rows, and walks over the tiles
-// with a stride: 16384 x 8192 x 4096 in 222 us (5.0 PFLOP/s), 8192 x 8192 x 16384 in 404 (5.4).  What bounds it is the
-// copies that feed it, 43 bytes a cycle into every SM beside the products: on operands that are there already a product of
-// 256 x 256 x 64 takes 169 cycles, here about 217; results that leave in the same time add to that for short sums
-// (16384 x 6400 x 1600: 86 us).
+// with a stride: 16384 x 8192 x 4096 in 205 us (5.4 PFLOP/s; 236 us back to back under the power limit),
+// 8192 x 8192 x 16384 in 369 (6.0).  What bounds it is the copies that feed it: a product of 256 x 256 x 64 takes 203
+// cycles with the copies of the next ones beside it, 43 bytes a cycle into every SM, and 169 on operands that are there
+// already; results that leave in the same time add to that (short sums: 16384 x 6400 x 1600 81 us, nothing stored 68).
 // Every byte of A goes to one SM and every byte of B's codes too (the tensor cores read the partner's half from its
 // shared memory); only B's scales go to both.
 constexpr int kPairStages = 5;
@@ -330,12 +315,10 @@ constexpr int kPairThreads = 448;
 constexpr int kPairOverlap = 128;
 static_assert(256 + kPairOverlap + kPairStages * kPairScaleColumns <= 512, "tensor memory has 512 columns");
 __device__ __forceinline__ uint32_t pair_sums_at(uint32_t round) { return round & 1 ? kPairOverlap : 0; }
-// full: this block's copies (all of the first block's; the second's scales); codes: the second block's codes, on the first
-// block's barrier; scaled: both blocks' scales are in tensor memory.
 struct alignas(16) PairShared {
-    unsigned long long full[kPairStages], codes[kPairStages], scaled[kPairStages], empty[kPairStages], sums_full, sums_empty, finished;
+    unsigned long long full[kPairStages], scaled[kPairStages], empty[kPairStages], sums_full, sums_empty, finished;
     uint32_t tmem;
-    int gave_up, partner_gave_up, partner_issued;
+    int gave_up;
 };
 constexpr int kTurnPitch = 33;                       // floats; a warp's 32 x 32 sums, turned so that lanes hold neighbours
 constexpr int kPairSmem = kPairStages * kPairStageBytes + 1024 + (int)sizeof(PairShared) + 8 * 32 * kTurnPitch * 4;
@@ -344,7 +327,6 @@ constexpr int kPairSmem = kPairStages * kPairStageBytes + 1024 + (int)sizeof(Pai
 // the first's tiles with a stride.  Where that leaves some pairs one short, these take `extra` of the second's each, about
 // as long as the one; what remains goes round all, beginning with them.
 struct PairArgs {
-    CUtensorMap codes_a[2], codes_b[2];      // of each product, for the second block's copies
     MatmulArgs product[2];
     long long tiles[2];
     int extra;
@@ -388,7 +370,7 @@ struct PairWalk {
 struct PairTile {
     long long i0;        // this block's first row of A
     long long j0;        // the pair's first row of B
-    int rows, cols;      // this block's rows that exist (0..128); the pair's columns: 256, or a multiple of 32 up to 128
+    int rows, cols;      // this block's rows that exist (0..128); the pair's columns, a multiple of 32
 };
 __device__ __forceinline__ PairTile pair_tile(const MatmulArgs &g, long long t, int rank)
 {
@@ -400,14 +382,14 @@ __device__ __forceinline__ PairTile pair_tile(const MatmulArgs &g, long long t, 
     p.i0 = in / width * 256 + rank * 128;
     p.j0 = (first + in % width) * 256;
     p.rows = (int)(g.m - p.i0 < 0 ? 0 : g.m - p.i0 < 128 ? g.m - p.i0 : 128);
-    p.cols = (int)(g.n - p.j0 <= 128 ? (g.n - p.j0 + 31) / 32 * 32 : 256);      // so that a block's half lies in one tile of B
+    p.cols = (int)(g.n - p.j0 < 256 ? (g.n - p.j0 + 31) / 32 * 32 : 256);
     return p;
 }
 
 // 128 bytes of each of a warp's 32 rows (lane = row, already of type T), turned through shared memory so that a store writes
 // whole lines; rows are 16-byte aligned.  With a lane storing 32-byte pieces of its own row the stores held the copies up:
-// 16384 x 6400 x 1600 to bfloat16 by 4 us in 88, and 3 more are saved where results leave the L2 before operands do; to
-// binary32 by 15 in 123, and 5.
+// 16384 x 6400 x 1600 to bfloat16 88 us, this way 84, and 81 where results leave the L2 before operands do; to binary32 123,
+// 108 and 103.
 template <typename T>
 __device__ __forceinline__ void store_lines(T *first, long long ld, int rows, int cols, const uint32_t *w, float *turn)
 {
@@ -468,13 +450,6 @@ __device__ __forceinline__ void round32(const uint32_t *v, uint32_t *w)
     }
 }
 
-// Waits for the last copies on a ring's barriers, `issued` stages having been started.
-__device__ __forceinline__ void drain_stages(unsigned long long *bars, int issued, const WaitLimit &limit)
-{
-    for (int q = issued > kPairStages ? issued - kPairStages : 0; q < issued; ++q)
-        mbar_drain(smem_addr(&bars[q % kPairStages]), (uint32_t)(q / kPairStages & 1), limit);
-}
-
 // Warp 0 copies tiles, warps 2 to 5 bring their scales to tensor memory, warp 1 of the first block issues the products,
 // warps 6 to 13 take the sums: four quarters of the rows, two halves of the columns.
 template <typename T, bool kTwo>
@@ -489,7 +464,6 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
     if (threadIdx.x == 0) {
         for (int s = 0; s < kPairStages; ++s) {
             mbar_init(smem_addr(&sh->full[s]), 1);
-            mbar_init(smem_addr(&sh->codes[s]), 1);
             mbar_init(smem_addr(&sh->scaled[s]), 8);       // four warps of both blocks
             mbar_init(smem_addr(&sh->empty[s]), 1);
         }
@@ -518,21 +492,18 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
         for (PairWalk<kTwo> walk(args); walk.more() && ok; walk.next()) {
             const MatmulArgs &g = args.product[walk.second()];
             const PairTile p = pair_tile(g, walk.tile(), rank);
-            // B: scales of the pair's up to two tiles to both blocks, codes by halves of the pair's columns.  Of the first block's
-            // rows those past the end are not copied.  The second block's codes go by whole tiles (lines past the end of
-            // a tile or of the matrix come as zeros, and none of them reach a result): these copies can arrive on the barrier
-            // of the block that issues the products, which so sees them land itself; with copies that arrive here,
-            // a release at cluster scope would have to follow every stage (16384 x 8192 x 4096: 415 us, this way 222).
+            // B: scales of the pair's up to two tiles to both blocks, codes by halves of the pair's columns; a half may
+            // begin in one tile and end in the next.  Rows past the end are neither copied nor stored.
             const long long exist = g.n - p.j0 < p.cols ? g.n - p.j0 : p.cols;
-            const int half = p.cols / 2, two = exist > 128;
+            const int half = p.cols / 2, b0 = rank * half, b1 = (int)(exist < b0 + half ? (exist > b0 ? exist : b0) : b0 + half);
+            const int two = exist > 128;
+            const int cut = b0 < 128 ? (b1 < 128 ? b1 : 128) : b0;      // b0 .. cut lie in the first tile, cut .. b1 in the second
             const long long next_b = (long long)g.tiles_k * kMxTileBytes;
             const uint8_t *a = g.a + p.i0 / 128 * next_b, *b = g.b + p.j0 / 128 * next_b;
-            const uint32_t bytes_a = p.rows == 0 ? 0 : rank == 0 ? kMxScaleBytes + 128 * (uint32_t)p.rows : kMxScaleBytes;
-            const uint32_t bytes_b = rank == 0 ? 128 * (uint32_t)(exist < half ? exist : half) : 0;
-            const uint32_t bytes = bytes_a + kMxScaleBytes * (1 + two) + bytes_b;
-            const uint32_t bytes_codes = (p.rows ? kMxCodeBytes : 0) + kMxCodeBytes;
-            const CUtensorMap *map_a = &args.codes_a[walk.second()], *map_b = &args.codes_b[walk.second()];
-            const int tile_a = (int)(p.i0 / 128 * g.tiles_k), tile_b = (int)((p.j0 / 128 + (half == 128)) * g.tiles_k), line_b = half & 127;
+            const uint32_t bytes_a = p.rows ? kMxScaleBytes + 128 * (uint32_t)p.rows : 0;
+            const uint32_t bytes_1 = 128 * (uint32_t)(cut - b0), bytes_2 = 128 * (uint32_t)(b1 - cut);
+            const uint32_t bytes = bytes_a + kMxScaleBytes * (1 + two) + bytes_1 + bytes_2;
+            const uint8_t *b_1 = b + kMxScaleBytes + b0 * 128, *b_2 = b + next_b + kMxScaleBytes + (cut - 128) * 128;
             for (int k = 0; k < g.tiles_k; ++k) {
                 ok = !(args.product[0].test_stop > 0 && issued >= args.product[0].test_stop) && warp_wait(smem_addr(&sh->empty[s]), parity ^ 1u, gave_up, limit);
                 if (!ok) break;
@@ -540,18 +511,14 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
                 const uint32_t dst_sf = dst + kMxTileBytes, dst_b = dst_sf + 2 * kMxScaleBytes;
                 expect_one(one, full, bytes);
                 if (bytes_a) bulk_load_one(one, dst, a, bytes_a, full);
-                if (rank == 0) {
-                    bulk_load_one(one, dst_b, b + kMxScaleBytes, bytes_b, full);
-                } else {
-                    const uint32_t codes = address_at(smem_addr(&sh->codes[s]), 0);
-                    expect_there_one(one, codes, bytes_codes);
-                    if (p.rows) load_lines_one(one, dst + kMxScaleBytes, map_a, 0, tile_a + k, codes);
-                    load_lines_one(one, dst_b, map_b, line_b, tile_b + k, codes);
-                }
+                if (bytes_1) bulk_load_one(one, dst_b, b_1, bytes_1, full);
+                if (bytes_2) bulk_load_one(one, dst_b + bytes_1, b_2, bytes_2, full);
                 bulk_load_one(one, dst_sf, b, kMxScaleBytes, full);
                 if (two) bulk_load_one(one, dst_sf + kMxScaleBytes, b + next_b, kMxScaleBytes, full);
                 a += kMxTileBytes;
                 b += kMxTileBytes;
+                b_1 += kMxTileBytes;
+                b_2 += kMxTileBytes;
                 ++issued;
                 if (++s == kPairStages) {
                     s = 0;
@@ -561,8 +528,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
         }
         // Everything has been read when this completes; after giving up, copies in flight land first.
         const bool done = warp_wait(smem_addr(&sh->finished), 0, gave_up, limit);
-        if (!done || *gave_up) drain_stages(sh->full, issued, limit);
-        if (rank == 1 && lane == 0) store_there(smem_addr(&sh->partner_issued), 0, issued);
+        if (!done || *gave_up)
+            for (int q = issued > kPairStages ? issued - kPairStages : 0; q < issued; ++q)
+                mbar_drain(smem_addr(&sh->full[q % kPairStages]), (uint32_t)(q / kPairStages & 1), limit);
     } else if (warp == 1 && rank == 0) {
         const uint32_t one = elect_one();
         int s = 0;
@@ -573,11 +541,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
             const PairTile p = pair_tile(g, walk.tile(), 0);
             const uint32_t desc = mma_desc(256, p.cols, 0);
             const uint32_t sums = tmem + pair_sums_at(round);
-            if (round > 0 && !warp_wait(smem_addr(&sh->sums_empty), (round - 1) & 1u, gave_up, limit)) break;
+            if (round > 0 && !warp_wait<true>(smem_addr(&sh->sums_empty), (round - 1) & 1u, gave_up, limit)) break;
             for (int k = 0; k < g.tiles_k; ++k) {
-                // Both blocks' scales are in tensor memory, which says that the first block's codes have landed; the second's
-                // are seen to land here.
-                if (!(ok = warp_wait(smem_addr(&sh->scaled[s]), parity, gave_up, limit) && warp_wait<true>(smem_addr(&sh->codes[s]), parity, gave_up, limit))) break;
+                // both blocks' copies have landed and their scales are in tensor memory
+                if (!(ok = warp_wait<true>(smem_addr(&sh->scaled[s]), parity, gave_up, limit))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t base_a = smem_addr(ring + s * kPairStageBytes), base_b = base_a + kMxTileBytes + 2 * kMxScaleBytes;
                 const uint32_t sf = tmem + 256 + kPairOverlap + s * kPairScaleColumns;
@@ -627,11 +594,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    // Only tensor memory is handed over to the other block here, in the pattern that the PTX ISA gives for it:
-                    // the stores waited for, tcgen05.fence::before_thread_sync, a relaxed arrival, a wait, and
-                    // tcgen05.fence::after_thread_sync ahead of the product that reads them.
-                    if (rank == 0) mbar_arrive(smem_addr(&sh->scaled[s]));
-                    else mbar_tell(smem_addr(&sh->scaled[s]), 0);
+                    // To the first block goes the news that this one's copies have landed, which the fence puts ahead of the
+                    // arrival, and that its scales are in tensor memory, which wait::st and the fences of tcgen05 do.
+                    // (A release at cluster scope instead: 16384 x 8192 x 4096 in 415 us for 205.)
+                    if (rank == 0) {
+                        mbar_arrive(smem_addr(&sh->scaled[s]));
+                    } else {
+                        release_shared();
+                        mbar_tell(smem_addr(&sh->scaled[s]), 0);
+                    }
                 }
                 if (++s == kPairStages) {
                     s = 0;
@@ -666,8 +637,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
                 if (pass == 0) {
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
-                    // The loads waited for and fenced, as for the scales above: only tensor memory is handed over, no release
-                    // needed (it would wait for the last tile's stores).
+                    // Only tensor memory is handed over: its loads have been waited for and fenced.
                     if (lane == 0) mbar_tell(smem_addr(&sh->sums_empty), 0);
                 }
                 constexpr int kAtOnce = 128 / (int)sizeof(T);
@@ -684,13 +654,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) mat
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (threadIdx.x == 0) store_there(smem_addr(&sh->partner_gave_up), (uint32_t)(rank ^ 1), *gave_up);
     cluster_sync();
-    if (*gave_up || sh->partner_gave_up) {      // the same in both blocks: the second block's codes in flight land before either leaves
-        if (rank == 0 && warp == 0) drain_stages(sh->codes, sh->partner_issued, limit);
-        __syncthreads();
-        cluster_sync();
-    }
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
@@ -765,44 +729,13 @@ void launch_small(const MatmulArgs &g, int splits, cudaStream_t s)
     cudaLaunchKernelEx(&cfg, kernel, g, splits, tiles_n);
 }
 
-// The codes of a form, 128 bytes a line, as [tile][line][byte], taken 128 lines at a time.  (With the tiles' rows and columns
-// as two dimensions the product took 237 us for 222.)
-cudaError_t code_lines(CUtensorMap *map, const uint8_t *form, long long rows, int tiles_k)
-{
-    static std::atomic<decltype(&cuTensorMapEncodeTiled)> encode{nullptr};
-    auto f = encode.load(std::memory_order_acquire);
-    if (!f) {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found);
-        if (e != cudaSuccess) return e;
-        if (found != cudaDriverEntryPointSuccess) return cudaErrorSymbolNotFound;
-        f = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(p);
-        encode.store(f, std::memory_order_release);
-    }
-    const cuuint64_t size[3] = {128, kMxTileRows, (cuuint64_t)tiles_k * (cuuint64_t)mx_tiles(rows, kMxTileRows)};
-    const cuuint64_t stride[2] = {128, kMxTileBytes};
-    const cuuint32_t box[3] = {128, kMxTileRows, 1}, step[3] = {1, 1, 1};
-    const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t *>(form) + kMxScaleBytes, size, stride, box, step,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
-}
-
 template <typename T, bool kTwo>
-cudaError_t launch_pairs(PairArgs &p, int sms, cudaStream_t s)
+void launch_pairs(const PairArgs &p, int sms, cudaStream_t s)
 {
     static SmemLimit limit;
-    cudaError_t e = limit.ensure(matmul_pair_kernel<T, kTwo>, kPairSmem);
-    for (int i = 0; i <= kTwo && e == cudaSuccess; ++i) {
-        const MatmulArgs &g = p.product[i];
-        e = code_lines(&p.codes_a[i], g.a, g.m, g.tiles_k);
-        if (e == cudaSuccess) e = code_lines(&p.codes_b[i], g.b, g.n, g.tiles_k);
-    }
-    if (e != cudaSuccess) return e;
+    if (limit.ensure(matmul_pair_kernel<T, kTwo>, kPairSmem) != cudaSuccess) return;       // the caller reports it
     const long long pairs = p.tiles[1] < sms / 2 ? p.tiles[1] : sms / 2;
     matmul_pair_kernel<T, kTwo><<<(unsigned)(2 * pairs), kPairThreads, kPairSmem, s>>>(p);
-    return cudaSuccess;
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------
@@ -1026,21 +959,20 @@ extern "C" zoa_status zoa_mx4_matmul(const void *a, const void *b, size_t m, siz
     st = product_args(me, a, b, m, n, k, out, dtype, ld, g, sms);
     if (st != ZOA_OK) return st;
     const ProductPlan plan = product_plan(g, sms);
-    cudaError_t e = cudaSuccess;
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
         if (plan.columns == 256) {
             PairArgs p{};
             p.product[0] = g;
             p.tiles[0] = p.tiles[1] = pair_tiles(g);
-            e = launch_pairs<T, false>(p, sms, s);
+            launch_pairs<T, false>(p, sms, s);
         } else if (plan.columns == 128) {
             launch_small<T, 128>(g, plan.splits, s);
         } else {
             launch_small<T, 64>(g, plan.splits, s);
         }
     });
-    return e == cudaSuccess ? ops_launched(me) : ops_fail(ZOA_ERR_CUDA, "%s: %s", me, cudaGetErrorString(e));
+    return ops_launched(me);
 }
 
 extern "C" size_t zoa_mx4_linear_work(size_t m, size_t n, size_t k)
@@ -1129,19 +1061,18 @@ extern "C" zoa_status zoa_mx4_linear_backward(const void *dy, int dy_type, size_
     if (st == ZOA_OK && k) st = zoa_mx4_quantize(dy, dy_type, m, n, ld_dy, dy_rows, dy_columns, stream);
     if (st == ZOA_OK && dx && dw && dx_type == dw_type && m && n && k) {
         // Both in one launch where that is no slower: small ones fill the SMs together (rounding and both products, 512 x 1024
-        // -> 4096: 25.7 -> 22.7 us, 1777 x 1001 -> 1333 30.8 -> 24.7), of large ones the last tiles of the longer sums run
-        // beside the others' (16384 x 1600 -> 6400: 237 -> 217).
+        // -> 4096: 25.0 -> 20.6 us, 1777 x 1001 -> 1333 31.8 -> 25.5), of large ones the last tiles of the longer sums run
+        // beside the others' (16384 x 1600 -> 6400: 219 -> 203).
         MatmulArgs of_x{}, of_w{};
         int sms = 0;
         st = product_args(me, work, wt, m, k, n, dx, dx_type, ld_dx, of_x, sms);
         if (st == ZOA_OK) st = product_args(me, dyt, xt, n, k, m, dw, dw_type, ld_dw, of_w, sms);
         if (st != ZOA_OK) return st;
         double together = 0.0;
-        PairArgs p = pair_both(of_x, of_w, sms, &together);
+        const PairArgs p = pair_both(of_x, of_w, sms, &together);
         if (together <= product_plan(of_x, sms).time + product_plan(of_w, sms).time) {
-            cudaError_t e = cudaSuccess;
-            with_type(dx_type, [&](auto t) { e = launch_pairs<decltype(t), true>(p, sms, static_cast<cudaStream_t>(stream)); });
-            return e == cudaSuccess ? ops_launched(me) : ops_fail(ZOA_ERR_CUDA, "%s: %s", me, cudaGetErrorString(e));
+            with_type(dx_type, [&](auto t) { launch_pairs<decltype(t), true>(p, sms, static_cast<cudaStream_t>(stream)); });
+            return ops_launched(me);
         }
     }
     if (st == ZOA_OK && dx) st = zoa_mx4_matmul(work, wt, m, k, n, dx, dx_type, ld_dx, stream);
