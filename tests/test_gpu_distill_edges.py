@@ -125,3 +125,15 @@ def test_pointers_that_are_not_aligned_are_refused():
         with pytest.raises(ZoaError) as e:
             call()
         assert e.value.status == B.ERR_ARG
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab,rows", [(100, 5), (6001, 40), (30001, 3), (50257, 700)])
+def test_backward_in_place_of_the_logits(vocab, rows, dtype):
+    p = problem(rows, vocab, 16, dtype, 8, tail=True, labels=True, T=2.0)
+    stats = distill_topk(**p, stats=True)[1]
+    scale = torch.linspace(-1, 2, rows, device="cuda")
+    grad = distill_topk_backward(scale, stats, **p)
+    z = p["logits"].clone()
+    assert distill_topk_backward(scale, stats, **dict(p, logits=z), out=z) is z
+    assert torch.equal(grad, z)
