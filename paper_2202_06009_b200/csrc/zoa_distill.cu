@@ -221,10 +221,13 @@ struct DistillShared {
 //
 // What bounds it, apart from device memory: exponentials, one per element and pass.  exp(z - m) is the square of
 // exp((z - m) / 2), so at temperature 2 the hard part needs none of its own (kPower 2), at temperature 1 it is the
-// soft part's (kPower 0, also where there is no hard part); other temperatures pay for both (kPower -1).
+// soft part's (kPower 0, also where there is no hard part); other temperatures pay for both (kPower -1).  8192 x 50257
+// bfloat16 with labels, loss alone and with the gradient: T = 1 138 and 312 us, T = 2 144 and 320, T = 1.5 or 4 218 and 440;
+// binary32 rows are bound by memory at any of them (4096 x 30522: 85 to 88, 208).
 //
-// Threads a row: 128 for the loss alone, where more rows in flight hide more (8192 x 50257: 151 us, 256 threads 172);
-// 256 with a gradient, where more rows in flight no longer fit L2 between the passes (334 us, 128 threads 404).
+// Threads a row: 128 for the loss alone, where more rows in flight hide more (8192 x 50257: 138 us, 256 threads 158;
+// 8192 x 2000: 35 and 62); 256 with a gradient, where more rows in flight no longer fit L2 between the passes (8192 x 50257
+// 312 us, 128 threads 391; 8192 x 30522 alike; on 8192 x 2000, all of whose rows fit, 128 would take 48 for 82).
 // kAlone: one block a row.
 template <typename T, int kPower, int kThreads, bool kAlone>
 __global__ void __launch_bounds__(kThreads, kThreadsPerSm / kThreads) distill_kernel(const DistillArgs a, const int cluster_blocks,
